@@ -464,6 +464,168 @@ int kvr_fork(const kvr_cache *src, const kvr_cache *dst, const int32_t *src_inde
 int kvr_append(const kvr_cache *cache, const int32_t *len, int32_t T, const void *k_new,
                const void *v_new, const int32_t *pos_new, hipStream_t stream);
 
+/*
+ * A KV cache held in 4 bits: a context that is read every step and hardly ever
+ * changes (the helper's full context, Sec. 3.1) in 0.28 to 0.31 of its bfloat16
+ * bytes.
+ *
+ *   data  : device memory of kvr_quant_cache_bytes() bytes, 16-byte aligned,
+ *           no initialisation needed. Units (sequence, layer, KV head) lie one
+ *           after the other, each in tiles of 32 slots; a tile holds 32 D bytes
+ *           of codes and 256 D / group of scales and offsets. The sequences i,
+ *           i + 1, .. of a cache are a cache of their own that starts i *
+ *           bytes / S further on.
+ *   group : 32 or 64 consecutive values of a row share a scale and an offset.
+ *
+ * A group with values x (a NaN taken as 0, all clamped to +-16384; every step
+ * rounded to nearest even in the stated type) is held as
+ *   z = float16(min x)
+ *   s = float16((max x - z) * (1.0f / 15.0f)) in float32, 0 where max x <= z
+ *   n = clamp(round_to_even((x - z) * (1.0f / s)), 0, 15) in float32, 0 where
+ *       s is 0
+ * and stands for z + s n. An appended row does not depend on its neighbours,
+ * and everything held is finite.
+ */
+typedef struct kvr_quant_cache {
+    void *data;
+    int32_t S, L, Hkv, cap, D;
+    int32_t group;
+} kvr_quant_cache;
+
+/* Bytes of a cache's data (0 for an invalid description; data is not read). */
+size_t kvr_quant_cache_bytes(const kvr_quant_cache *cache);
+
+/*
+ * kvr_quant_append -- rows quantised and appended to a cache held in 4 bits: an
+ * accepted step that joins the context (App. C; Alg. 1), or a prompt.
+ *
+ *   len       : [dst->S] int32 device, live slots before the append (read only).
+ *   src       : the rows, a cache of float32 or bfloat16 with dst's L, Hkv and
+ *               D (its pos is not read). A packed array [S][L][Hkv][T][D] is a
+ *               cache of cap T; the own cache of a candidate is one as it
+ *               stands.
+ *   src_index : NULL (sequence s takes src sequence s; src->S == dst->S), or
+ *               [dst->S] int32 device: the src sequence of each. Destinations
+ *               with an index outside [0, src->S) are skipped; an index may
+ *               occur more than once.
+ *   count     : NULL (src->cap rows), or [dst->S] int32 device: slots 0 ..
+ *               count[s] - 1 of the source, clamped to [0, src->cap], go to
+ *               slots len[s], len[s] + 1, ...
+ * Slots at or beyond cap are not written, and no other slot changes. The caller
+ * keeps the new lengths.
+ * Errors: KVR_EINVAL (pointer, shape, alignment), KVR_EUNSUPPORTED (dtype, D,
+ * group, grid), KVR_EHIP.
+ */
+int kvr_quant_append(const kvr_quant_cache *dst, const int32_t *len, const kvr_cache *src,
+                     const int32_t *src_index, const int32_t *count, hipStream_t stream);
+
+/*
+ * kvr_quant_read -- slots of a cache held in 4 bits given back as the values
+ * they stand for (z + s n in float32, rounded to dst's dtype), for what works
+ * on whole rows: window scores, eviction, a fork into an evicted cache.
+ *
+ *   dst       : a cache of float32 or bfloat16 with src's L, Hkv and D; slots 0
+ *               .. len[s] - 1 of sequence s are written (at most src->cap and
+ *               dst->cap of them), k and v only.
+ *   src_index : as for kvr_quant_append (NULL needs src->S == dst->S).
+ *   len       : [dst->S] int32 device.
+ * Errors: as kvr_quant_append.
+ */
+int kvr_quant_read(const kvr_quant_cache *src, const kvr_cache *dst, const int32_t *src_index,
+                   const int32_t *len, hipStream_t stream);
+
+/*
+ * kvr_quant_attn -- grouped-query attention of one or several query tokens per
+ * sequence over a context held in 4 bits and the sequence's own cache: a decode
+ * step of the full-context helper (Sec. 3.1), or one pass of a model over
+ * drafted tokens.
+ *
+ * The tokens of sequence s are the ctx_len[s / C] live slots of its context, C
+ * = S / ctx->S, and then the len[s] live slots of its own cache. The nq query
+ * tokens are the last nq of these; query token t attends to all but the last nq
+ * - 1 - t tokens. A query token that sees none gives a row of zeros.
+ *
+ *   ctx, ctx_len : the contexts, [ctx->S] int32 device live lengths, 0 and up.
+ *   own, len  : NULL and NULL (the context alone holds the tokens; S is ctx->S),
+ *               or the sequences' own cache of `dtype`, with ctx's L, Hkv and D
+ *               and S a multiple of ctx->S, and [S] int32 device live lengths
+ *               including the nq new tokens where k_new is given.
+ *   q, out    : [S][L][Hq][nq][D] of `dtype`, Hq = G * Hkv, 1 <= G <= 16.
+ *   dtype     : KVR_BF16, or KVR_F32 (a vector kernel, meant for validation).
+ *   k_new, v_new : [S][L][Hkv][nq][D] rows of the query tokens, written to own
+ *               slots len[s] - nq .. len[s] - 1 (those below 0 are not written,
+ *               but attended to by nobody) and attended to in the same call; or
+ *               both NULL when the tokens are already stored.
+ *   new_pos   : NULL, or [S][nq] int32 positions of the new tokens, stored into
+ *               own->pos; needs k_new.
+ *   workspace : device scratch of kvr_quant_attn_workspace_size() bytes,
+ *               16-byte aligned, no initialisation; NULL/0 where that is 0.
+ * Lengths beyond the caches' slots count as full, negative ones as 0.
+ * Results do not depend on the order in which the GPU runs the work, and a row
+ * that a query token does not see does not reach its output, whatever it holds.
+ * Errors: KVR_EINVAL (pointer, shape, alignment), KVR_EUNSUPPORTED (dtype, D,
+ * group, G > 16, nq > 64, grid), KVR_EWORKSPACE, KVR_EHIP.
+ */
+int kvr_quant_attn(const kvr_quant_cache *ctx, const int32_t *ctx_len, const kvr_cache *own,
+                   const int32_t *len, const void *q, int32_t dtype, int32_t Hq, int32_t nq,
+                   float scale, const void *k_new, const void *v_new, const int32_t *new_pos,
+                   void *out, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of kvr_quant_attn (0 for invalid shapes; pointers, own->S and
+ * ctx->S aside, are not read). They depend on the shapes and caps, not on the
+ * lengths. */
+size_t kvr_quant_attn_workspace_size(const kvr_quant_cache *ctx, const kvr_cache *own, int32_t dtype,
+                                     int32_t Hq, int32_t nq);
+
+/*
+ * kvr_verify_draft -- drafted tokens checked against the target model's
+ * distribution, and the next token drawn, so that the tokens of a sequence are
+ * distributed as if the target had sampled them one by one (speculative
+ * sampling).
+ *
+ * P_t and Q_t are the distributions kvr_logit_entropy_sample draws from
+ * (temperature, top_k with ties to the lower id, top_p, renormalised) for the
+ * target's and the draft's logits at position t. Token x_t stands while
+ *   u_accept[t] * Q_t(x_t) < P_t(x_t).
+ * At the first that does not, the next token is drawn from max(P_t - Q_t, 0),
+ * or from P_t where that is 0 everywhere; after n_draft[s] tokens that stand it
+ * is drawn from P at position n_draft[s]. The draw takes the first token, by
+ * falling logit, whose cumulative mass exceeds u_draw[s] times the whole. All
+ * of this is computed in float64.
+ *
+ *   logits    : [S][T + 1][ld] of `dtype`, the first V of each row: row t is the
+ *               target's prediction of drafted token t.
+ *   draft_logits : [S][T][ldd] of `dtype`, the first Vd <= V of each row, the
+ *               distributions the tokens were drawn from; or NULL with Vd = 0:
+ *               tokens that were looked up, Q_t all on x_t.
+ *   draft_tokens : [S][T] int32 device. A token outside [0, V) never stands.
+ *   n_draft   : NULL (T each), or [S] int32 device, tokens drafted for each
+ *               sequence, clamped to [0, T]; later rows are not read.
+ *   sampler, draft_sampler : temperature, top_k and top_p of the two (seed and
+ *               step are not used); draft_sampler NULL: the same.
+ *   u_accept  : [S][T] float32, u_draw: [S] float32, uniforms in [0, 1).
+ *   accepted  : [S] int32 output, how many drafted tokens stand.
+ *   tokens    : [S][T + 1] int32 output: those, the next token, then -1.
+ *   len, len_out : NULL and NULL, or [S] int32 device: len_out[s] = len[s] -
+ *               (n_draft[s] - accepted[s]), the live length of a cache that
+ *               held the query tokens. They may be the same array.
+ *   workspace : device scratch of kvr_verify_draft_workspace_size() bytes,
+ *               16-byte aligned, no initialisation.
+ * Rows must hold at least one finite logit and no +inf; -inf has no mass. A NaN
+ * counts as absent.
+ * Errors: KVR_EINVAL (pointer, shape, sampler), KVR_EUNSUPPORTED (dtype, T >
+ * 32, V > 2^30, S (2 T + 1) > 2^20), KVR_EWORKSPACE, KVR_EHIP.
+ */
+int kvr_verify_draft(const void *logits, int32_t V, int64_t ld, const void *draft_logits, int32_t Vd,
+                     int64_t ldd, int32_t dtype, int32_t S, int32_t T, const int32_t *draft_tokens,
+                     const int32_t *n_draft, const kvr_sampler *sampler,
+                     const kvr_sampler *draft_sampler, const float *u_accept, const float *u_draw,
+                     int32_t *accepted, int32_t *tokens, const int32_t *len, int32_t *len_out,
+                     void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* top_k: the larger of the two samplers'. 0 for invalid shapes. */
+size_t kvr_verify_draft_workspace_size(int32_t S, int32_t T, int32_t V, int32_t Vd, int32_t top_k);
+
 #ifdef __cplusplus
 }
 #endif

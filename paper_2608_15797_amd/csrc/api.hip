@@ -544,3 +544,222 @@ int kvr_decode_attn_entropy_sample(const kvr_cache *cache, const kvr_prefix *pre
 }
 
 }  // extern "C"
+
+namespace {
+
+int check_quant(const kvr_quant_cache *c) {
+  if (!c) return fail(KVR_EINVAL, "quant cache is NULL");
+  if (c->S <= 0 || c->L <= 0 || c->Hkv <= 0 || c->cap <= 0)
+    return fail(KVR_EINVAL, "quant cache dims must be positive (S=%d L=%d Hkv=%d cap=%d)", c->S, c->L, c->Hkv, c->cap);
+  if (c->D != 64 && c->D != 128) return fail(KVR_EUNSUPPORTED, "head_dim %d is not 64 or 128", c->D);
+  if (c->group != 32 && c->group != 64) return fail(KVR_EUNSUPPORTED, "group %d is not 32 or 64", c->group);
+  if ((double)c->S * c->L * c->Hkv > 2147483647.0) return fail(KVR_EUNSUPPORTED, "S*L*Hkv exceeds the launch grid");
+  return KVR_OK;
+}
+
+int check_quant_data(const kvr_quant_cache *c) {
+  const int st = check_quant(c);
+  if (st) return st;
+  if (!c->data) return fail(KVR_EINVAL, "quant cache data is NULL");
+  if (!aligned16(c->data)) return fail(KVR_EINVAL, "quant cache data not 16-byte aligned");
+  return KVR_OK;
+}
+
+long quant_tiles(int cap) { return ((long)cap + kvr::kQuantTile - 1) / kvr::kQuantTile; }
+
+// The rows of a cache beside a 4-bit one.
+int check_rows(const kvr_quant_cache *c, const kvr_cache *rows, const char *what) {
+  int G = 0;
+  const int st = check_cache(rows, 0, &G);
+  if (st) return st;
+  if (rows->L != c->L || rows->Hkv != c->Hkv || rows->D != c->D)
+    return fail(KVR_EINVAL, "%s and the quant cache differ in L, Hkv or D", what);
+  return KVR_OK;
+}
+
+// Shapes of an attention call into p (no pointers but what says whether own is given).
+int quant_attn_shapes(const kvr_quant_cache *ctx, const kvr_cache *own, int32_t dtype, int32_t Hq, int32_t nq,
+                      kvr::QuantAttnParams *p) {
+  int st = check_quant(ctx);
+  if (st) return st;
+  if (dtype != KVR_F32 && dtype != KVR_BF16)
+    return fail(KVR_EUNSUPPORTED, "dtype %d is not KVR_F32 or KVR_BF16", dtype);
+  if (Hq <= 0 || Hq % ctx->Hkv != 0) return fail(KVR_EINVAL, "Hq=%d is not a positive multiple of Hkv=%d", Hq, ctx->Hkv);
+  if (Hq / ctx->Hkv > 16) return fail(KVR_EUNSUPPORTED, "G=%d query heads per KV head exceeds 16", Hq / ctx->Hkv);
+  if (nq <= 0) return fail(KVR_EINVAL, "nq must be positive");
+  if (nq > 64) return fail(KVR_EUNSUPPORTED, "nq=%d query tokens exceeds 64", nq);
+  if (own) {
+    if (own->L != ctx->L || own->Hkv != ctx->Hkv || own->D != ctx->D)
+      return fail(KVR_EINVAL, "own and the context differ in L, Hkv or D");
+    if (own->dtype != dtype) return fail(KVR_EINVAL, "own has dtype %d, the queries %d", own->dtype, dtype);
+    if (own->S <= 0 || own->cap <= 0 || own->S % ctx->S != 0)
+      return fail(KVR_EINVAL, "S=%d is not a positive multiple of the %d contexts, or cap=%d", own->S, ctx->S, own->cap);
+  }
+  *p = kvr::QuantAttnParams{};
+  p->P = ctx->S; p->L = ctx->L; p->Hkv = ctx->Hkv; p->cap = ctx->cap; p->D = ctx->D; p->group = ctx->group;
+  p->ntiles = quant_tiles(ctx->cap);
+  p->S = own ? own->S : ctx->S;
+  p->C = p->S / p->P;
+  p->ocap = own ? own->cap : 0;
+  p->dtype = dtype; p->Hq = Hq; p->G = Hq / ctx->Hkv; p->nq = nq;
+  if ((double)p->S * p->L * Hq * nq > 2147483647.0) return fail(KVR_EUNSUPPORTED, "S*L*Hq*nq exceeds the launch grid");
+  return KVR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kvr_quant_cache_bytes(const kvr_quant_cache *cache) {
+  if (check_quant(cache)) return 0;
+  return (size_t)cache->S * cache->L * cache->Hkv * quant_tiles(cache->cap) *
+         kvr::quant_tile_bytes(cache->D, cache->group);
+}
+
+int kvr_quant_append(const kvr_quant_cache *dst, const int32_t *len, const kvr_cache *src,
+                     const int32_t *src_index, const int32_t *count, hipStream_t stream) {
+  int st = check_quant_data(dst);
+  if (st) return st;
+  st = check_rows(dst, src, "src");
+  if (st) return st;
+  if (!len) return fail(KVR_EINVAL, "len is required");
+  if (!src_index && src->S != dst->S)
+    return fail(KVR_EINVAL, "src has S=%d, dst S=%d, and there is no src_index", src->S, dst->S);
+  const double groups = (double)dst->S * dst->L * dst->Hkv * ((double)(src->cap / kvr::kQuantTile) + 2);
+  if (groups > 2147483647.0) return fail(KVR_EUNSUPPORTED, "%d rows of %d units exceed the launch grid", src->cap,
+                                         dst->S * dst->L * dst->Hkv);
+  kvr::QuantAppendParams p{};
+  p.data = dst->data; p.S = dst->S; p.L = dst->L; p.Hkv = dst->Hkv; p.cap = dst->cap; p.D = dst->D;
+  p.group = dst->group; p.ntiles = quant_tiles(dst->cap); p.len = len;
+  p.k = src->k; p.v = src->v; p.S_src = src->S; p.T = src->cap; p.dtype = src->dtype;
+  p.src_index = src_index; p.count = count;
+  return hip_status(kvr::launch_quant_append(p, stream), "kvr_quant_append launch");
+}
+
+int kvr_quant_read(const kvr_quant_cache *src, const kvr_cache *dst, const int32_t *src_index,
+                   const int32_t *len, hipStream_t stream) {
+  int st = check_quant_data(src);
+  if (st) return st;
+  st = check_rows(src, dst, "dst");
+  if (st) return st;
+  if (!len) return fail(KVR_EINVAL, "len is required");
+  if (!src_index && src->S != dst->S)
+    return fail(KVR_EINVAL, "src has S=%d, dst S=%d, and there is no src_index", src->S, dst->S);
+  const double groups = (double)dst->S * dst->L * dst->Hkv * ((double)quant_tiles(dst->cap) + 1);
+  if (groups > 2147483647.0) return fail(KVR_EUNSUPPORTED, "%d slots of %d units exceed the launch grid", dst->cap,
+                                         dst->S * dst->L * dst->Hkv);
+  kvr::QuantReadParams p{};
+  p.data = src->data; p.S_src = src->S; p.L = src->L; p.Hkv = src->Hkv; p.cap = src->cap; p.D = src->D;
+  p.group = src->group; p.ntiles = quant_tiles(src->cap);
+  p.k = dst->k; p.v = dst->v; p.S = dst->S; p.cap_dst = dst->cap; p.dtype = dst->dtype;
+  p.src_index = src_index; p.len = len;
+  return hip_status(kvr::launch_quant_read(p, stream), "kvr_quant_read launch");
+}
+
+size_t kvr_quant_attn_workspace_size(const kvr_quant_cache *ctx, const kvr_cache *own, int32_t dtype,
+                                     int32_t Hq, int32_t nq) {
+  kvr::QuantAttnParams p;
+  if (quant_attn_shapes(ctx, own, dtype, Hq, nq, &p)) return 0;
+  return kvr::quant_attn_workspace_bytes(p);
+}
+
+int kvr_quant_attn(const kvr_quant_cache *ctx, const int32_t *ctx_len, const kvr_cache *own,
+                   const int32_t *len, const void *q, int32_t dtype, int32_t Hq, int32_t nq,
+                   float scale, const void *k_new, const void *v_new, const int32_t *new_pos,
+                   void *out, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  int st = check_quant_data(ctx);
+  if (st) return st;
+  if (own) {
+    st = check_rows(ctx, own, "own");
+    if (st) return st;
+  }
+  kvr::QuantAttnParams p;
+  st = quant_attn_shapes(ctx, own, dtype, Hq, nq, &p);
+  if (st) return st;
+  if (!ctx_len || !q || !out) return fail(KVR_EINVAL, "ctx_len, q and out are required");
+  if ((own == nullptr) != (len == nullptr)) return fail(KVR_EINVAL, "own and len must both be given or both be NULL");
+  if ((k_new == nullptr) != (v_new == nullptr))
+    return fail(KVR_EINVAL, "k_new and v_new must both be given or both be NULL");
+  if (k_new && !own) return fail(KVR_EINVAL, "k_new needs an own cache");
+  if (new_pos && !(k_new && own->pos)) return fail(KVR_EINVAL, "new_pos needs k_new and own->pos");
+  if (!aligned16(q) || !aligned16(out)) return fail(KVR_EINVAL, "q/out not 16-byte aligned");
+  if (k_new && (!aligned16(k_new) || !aligned16(v_new))) return fail(KVR_EINVAL, "k_new/v_new not 16-byte aligned");
+  p.data = ctx->data; p.ctx_len = ctx_len;
+  if (own) {
+    p.ok = own->k; p.ov = own->v; p.pos = own->pos;
+  }
+  p.len = len; p.q = q; p.out = out; p.scale = scale;
+  p.k_new = k_new; p.v_new = v_new; p.new_pos = new_pos;
+  const size_t need = kvr::quant_attn_workspace_bytes(p);
+  if (need) {
+    if (!workspace || workspace_bytes < need)
+      return fail(KVR_EWORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+    if (!aligned16(workspace)) return fail(KVR_EINVAL, "workspace not 16-byte aligned");
+    p.ws = static_cast<float *>(workspace);
+  }
+  return hip_status(kvr::launch_quant_attn(p, stream), "kvr_quant_attn launch");
+}
+
+}  // extern "C"
+
+namespace {
+
+constexpr int kVerifyMaxDraft = 32;
+
+int verify_shapes(int32_t S, int32_t T, int32_t V, int32_t Vd) {
+  if (S <= 0 || T <= 0 || V <= 0 || Vd < 0 || Vd > V)
+    return fail(KVR_EINVAL, "need S > 0, T > 0, V > 0, 0 <= Vd <= V (S=%d T=%d V=%d Vd=%d)", S, T, V, Vd);
+  if (T > kVerifyMaxDraft) return fail(KVR_EUNSUPPORTED, "T=%d drafted tokens exceeds %d", T, kVerifyMaxDraft);
+  if (V > (1 << 30)) return fail(KVR_EUNSUPPORTED, "V=%d exceeds 2^30", V);
+  if ((double)S * (2 * T + 1) > (double)(1 << 20))
+    return fail(KVR_EUNSUPPORTED, "S=%d sequences of T=%d are more than 2^20 rows", S, T);
+  return KVR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kvr_verify_draft_workspace_size(int32_t S, int32_t T, int32_t V, int32_t Vd, int32_t top_k) {
+  if (verify_shapes(S, T, V, Vd) || top_k < 1 || top_k > kvr::kTopKMax) return 0;
+  return kvr::verify_workspace_bytes(S, T, V, Vd, top_k);
+}
+
+int kvr_verify_draft(const void *logits, int32_t V, int64_t ld, const void *draft_logits, int32_t Vd,
+                     int64_t ldd, int32_t dtype, int32_t S, int32_t T, const int32_t *draft_tokens,
+                     const int32_t *n_draft, const kvr_sampler *sampler,
+                     const kvr_sampler *draft_sampler, const float *u_accept, const float *u_draw,
+                     int32_t *accepted, int32_t *tokens, const int32_t *len, int32_t *len_out,
+                     void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (!logits || !draft_tokens || !u_accept || !u_draw || !accepted || !tokens)
+    return fail(KVR_EINVAL, "logits, draft_tokens, u_accept, u_draw, accepted and tokens are required");
+  if (dtype != KVR_F32 && dtype != KVR_BF16) return fail(KVR_EUNSUPPORTED, "dtype %d", dtype);
+  int st = verify_shapes(S, T, V, Vd);
+  if (st) return st;
+  if ((draft_logits == nullptr) != (Vd == 0)) return fail(KVR_EINVAL, "draft_logits and Vd must both be given or be NULL and 0");
+  if (ld < V || (draft_logits && ldd < Vd))
+    return fail(KVR_EINVAL, "need ld >= V and ldd >= Vd (ld=%ld ldd=%ld)", (long)ld, (long)ldd);
+  if ((len == nullptr) != (len_out == nullptr)) return fail(KVR_EINVAL, "len and len_out must both be given or both be NULL");
+  if (!sampler) return fail(KVR_EINVAL, "sampler is required");
+  const kvr_sampler *ds = draft_sampler ? draft_sampler : sampler;
+  st = check_sampler(sampler);
+  if (!st) st = check_sampler(ds);
+  if (st) return st;
+  if (!std::isfinite(sampler->temperature) || !std::isfinite(ds->temperature))
+    return fail(KVR_EINVAL, "temperature must be finite");
+  const int k = sampler->top_k > ds->top_k ? sampler->top_k : ds->top_k;
+  const size_t need = kvr::verify_workspace_bytes(S, T, V, Vd, k);
+  if (!workspace || workspace_bytes < need)
+    return fail(KVR_EWORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+  if (!aligned16(workspace)) return fail(KVR_EINVAL, "workspace not 16-byte aligned");
+  kvr::VerifyParams p{};
+  p.logits = logits; p.draft = draft_logits; p.dtype = dtype; p.S = S; p.T = T; p.V = V; p.Vd = Vd;
+  p.ld = ld; p.ldd = ldd; p.tok = draft_tokens; p.n_draft = n_draft;
+  p.top_k = sampler->top_k; p.temp = sampler->temperature; p.top_p = sampler->top_p;
+  p.top_kd = ds->top_k; p.tempd = ds->temperature; p.top_pd = ds->top_p;
+  p.u_accept = u_accept; p.u_draw = u_draw; p.accepted = accepted; p.tokens = tokens;
+  p.len = len; p.len_out = len_out; p.ws = static_cast<uint64_t *>(workspace);
+  return hip_status(kvr::launch_verify_draft(p, stream), "kvr_verify_draft launch");
+}
+
+}  // extern "C"

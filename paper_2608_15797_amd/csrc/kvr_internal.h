@@ -176,4 +176,69 @@ struct AppendParams {
 };
 hipError_t launch_append(const AppendParams &p, hipStream_t stream);
 
+// The 4-bit cache: slots in tiles of kQuantTile (quant_common.h).
+constexpr int kQuantTile = 32;
+constexpr float kQuantLimit = 16384.f;
+inline size_t quant_tile_bytes(int D, int group) { return (size_t)32 * D + 256 * (D / group); }
+
+struct QuantAppendParams {
+  void *data;
+  int S, L, Hkv, cap, D, group;
+  long ntiles;
+  const int32_t *len;
+  const void *k, *v;  // [S_src][L][Hkv][T][D] of dtype
+  int S_src, T, dtype;
+  const int32_t *src_index, *count;  // NULL: the same sequence; T rows
+};
+hipError_t launch_quant_append(const QuantAppendParams &p, hipStream_t stream);
+
+struct QuantReadParams {
+  const void *data;
+  int S_src, L, Hkv, cap, D, group;
+  long ntiles;
+  void *k, *v;  // [S][L][Hkv][cap_dst][D] of dtype
+  int S, cap_dst, dtype;
+  const int32_t *src_index, *len;
+};
+hipError_t launch_quant_read(const QuantReadParams &p, hipStream_t stream);
+
+struct QuantAttnParams {
+  const void *data;  // context [P][L][Hkv] units
+  int P, L, Hkv, cap, D, group;
+  long ntiles;
+  const int32_t *ctx_len;
+  // own rows [S][L][Hkv][ocap][D]; ok == NULL: none (S == P)
+  void *ok, *ov;
+  int32_t *pos;
+  int S, C, ocap;  // C = S / P
+  const int32_t *len;
+  int dtype, Hq, G, nq;
+  const void *q;  // [S][L][Hq][nq][D]
+  void *out;
+  float scale;
+  const void *k_new, *v_new;  // [S][L][Hkv][nq][D], or NULL
+  const int32_t *new_pos;     // [S][nq], or NULL
+  float *ws;
+};
+size_t quant_attn_workspace_bytes(const QuantAttnParams &p);
+hipError_t launch_quant_attn(const QuantAttnParams &p, hipStream_t stream);
+
+// Drafted tokens checked against the target's distribution.
+struct VerifyParams {
+  const void *logits, *draft;  // [S][T + 1][ld], [S][T][ldd] or NULL
+  int dtype, S, T, V, Vd;
+  int64_t ld, ldd;
+  const int32_t *tok, *n_draft;
+  int top_k, top_kd;
+  float temp, top_p, tempd, top_pd;
+  const float *u_accept, *u_draw;
+  int32_t *accepted, *tokens;
+  const int32_t *len;
+  int32_t *len_out;
+  uint64_t *ws;
+  int splits;
+};
+size_t verify_workspace_bytes(int S, int T, int V, int Vd, int top_k);
+hipError_t launch_verify_draft(const VerifyParams &p, hipStream_t stream);
+
 }  // namespace kvr

@@ -27,7 +27,9 @@ EXPORTS = ("kvr_strerror", "kvr_last_error", "kvr_decode_attn", "kvr_decode_attn
            "kvr_logit_entropy_workspace_size", "kvr_fork", "kvr_append",
            "kvr_logit_entropy_sample", "kvr_logit_entropy_sample_workspace_size",
            "kvr_redundancy_scores", "kvr_logit_entropy_batch", "kvr_logit_entropy_batch_workspace_size",
-           "kvr_logit_entropy_batch_noalloc", "kvr_decode_attn_entropy", "kvr_decode_attn_entropy_sample")
+           "kvr_logit_entropy_batch_noalloc", "kvr_decode_attn_entropy", "kvr_decode_attn_entropy_sample",
+           "kvr_quant_cache_bytes", "kvr_quant_append", "kvr_quant_read", "kvr_quant_attn",
+           "kvr_quant_attn_workspace_size", "kvr_verify_draft", "kvr_verify_draft_workspace_size")
 
 
 class KvrError(RuntimeError):
@@ -60,6 +62,11 @@ class c_logit_set(ctypes.Structure):
     _fields_ = [("logits", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("R", ctypes.c_int32),
                 ("V", ctypes.c_int32), ("ld", ctypes.c_int64), ("inv_temp", ctypes.c_float),
                 ("H", ctypes.c_void_p), ("det", ctypes.POINTER(c_detector))]
+
+
+class c_quant_cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("S", ctypes.c_int32), ("L", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("cap", ctypes.c_int32), ("D", ctypes.c_int32), ("group", ctypes.c_int32)]
 
 
 class c_sampler(ctypes.Structure):
@@ -116,6 +123,22 @@ def _load():
     lib.kvr_fork.restype = ctypes.c_int
     lib.kvr_append.argtypes = [P(c_cache), vp, i32, vp, vp, vp, vp]
     lib.kvr_append.restype = ctypes.c_int
+    lib.kvr_quant_cache_bytes.argtypes = [P(c_quant_cache)]
+    lib.kvr_quant_cache_bytes.restype = sz
+    lib.kvr_quant_append.argtypes = [P(c_quant_cache), vp, P(c_cache), vp, vp, vp]
+    lib.kvr_quant_append.restype = ctypes.c_int
+    lib.kvr_quant_read.argtypes = [P(c_quant_cache), P(c_cache), vp, vp, vp]
+    lib.kvr_quant_read.restype = ctypes.c_int
+    lib.kvr_quant_attn.argtypes = [P(c_quant_cache), vp, P(c_cache), vp, vp, i32, i32, i32, f32, vp, vp, vp, vp, vp,
+                                   sz, vp]
+    lib.kvr_quant_attn.restype = ctypes.c_int
+    lib.kvr_quant_attn_workspace_size.argtypes = [P(c_quant_cache), P(c_cache), i32, i32, i32]
+    lib.kvr_quant_attn_workspace_size.restype = sz
+    lib.kvr_verify_draft.argtypes = [vp, i32, i64, vp, i32, i64, i32, i32, i32, vp, vp, P(c_sampler), P(c_sampler),
+                                     vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.kvr_verify_draft.restype = ctypes.c_int
+    lib.kvr_verify_draft_workspace_size.argtypes = [i32, i32, i32, i32, i32]
+    lib.kvr_verify_draft_workspace_size.restype = sz
     return lib
 
 
@@ -452,3 +475,119 @@ def redundancy_scores(cache: Cache, len_: torch.Tensor, importance: torch.Tensor
     rc = lib.kvr_redundancy_scores(ctypes.byref(cc), _ptr(len_), _ptr(importance), ctypes.byref(pol),
                                    float(lam), int(pool), _ptr(out), _stream(stream))
     _check(rc, "kvr_redundancy_scores")
+
+
+@dataclass
+class QuantCache:
+    """KV cache held in 4 bits: data[S][L][Hkv][tiles][bytes of a tile of 32 slots], uint8."""
+    data: torch.Tensor
+    cap: int
+    D: int
+    group: int = 32
+
+    @staticmethod
+    def empty(S, L, Hkv, cap, D, group=32, device="cuda"):
+        n = int(lib.kvr_quant_cache_bytes(ctypes.byref(c_quant_cache(None, S, L, Hkv, cap, D, group))))
+        if n == 0:
+            raise ValueError((lib.kvr_last_error() or b"").decode())
+        tiles = (cap + 31) // 32
+        return QuantCache(torch.empty((S, L, Hkv, tiles, n // (S * L * Hkv * tiles)), dtype=torch.uint8,
+                                      device=device), cap, D, group)
+
+    def sequences(self, a: int, b: int) -> "QuantCache":
+        """Sequences a .. b - 1, the same memory."""
+        return QuantCache(self.data[a:b], self.cap, self.D, self.group)
+
+    def c(self) -> c_quant_cache:
+        S, L, Hkv = self.data.shape[:3]
+        assert self.data.is_contiguous() and self.data.dtype == torch.uint8
+        cc = c_quant_cache(self.data.data_ptr(), S, L, Hkv, self.cap, self.D, self.group)
+        assert int(lib.kvr_quant_cache_bytes(ctypes.byref(cc))) == self.data.numel()
+        return cc
+
+
+def _ints(t: Optional[torch.Tensor], n: int):
+    assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n)
+    return _ptr(t)
+
+
+def quant_append(dst: QuantCache, len_: torch.Tensor, src: Cache, src_index: Optional[torch.Tensor] = None,
+                 count: Optional[torch.Tensor] = None, stream=None) -> None:
+    """kvr_quant_append: the first count[s] (all) rows of src sequence src_index[s] (s) to slots len[s] .. of dst."""
+    qc, sc = dst.c(), src.c()
+    rc = lib.kvr_quant_append(ctypes.byref(qc), _ints(len_, qc.S), ctypes.byref(sc), _ints(src_index, qc.S),
+                              _ints(count, qc.S), _stream(stream))
+    _check(rc, "kvr_quant_append")
+
+
+def quant_read(src: QuantCache, dst: Cache, len_: torch.Tensor, src_index: Optional[torch.Tensor] = None,
+               stream=None) -> None:
+    """kvr_quant_read: slots 0 .. len[s] - 1 of src sequence src_index[s] (s), as values, to sequence s of dst."""
+    qc, dc = src.c(), dst.c()
+    rc = lib.kvr_quant_read(ctypes.byref(qc), ctypes.byref(dc), _ints(src_index, dc.S), _ints(len_, dc.S),
+                            _stream(stream))
+    _check(rc, "kvr_quant_read")
+
+
+def quant_attn_workspace_size(ctx: QuantCache, own: Optional[Cache], Hq: int, nq: int = 1,
+                              dtype=torch.bfloat16) -> int:
+    qc = ctx.c()
+    oc = own.c() if own is not None else None
+    return int(lib.kvr_quant_attn_workspace_size(ctypes.byref(qc), ctypes.byref(oc) if oc else None,
+                                                 dtype_code(dtype), Hq, nq))
+
+
+def quant_attn(ctx: QuantCache, ctx_len: torch.Tensor, q: torch.Tensor, out: torch.Tensor, scale: float,
+               own: Optional[Cache] = None, len_: Optional[torch.Tensor] = None, k_new=None, v_new=None,
+               new_pos=None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """kvr_quant_attn: q[S][L][Hq][nq][D] -> out, over the 4-bit context and the own cache, to which
+    k_new/v_new [S][L][Hkv][nq][D] are appended at len - nq."""
+    qc = ctx.c()
+    oc = own.c() if own is not None else None
+    S = oc.S if oc else qc.S
+    for t in (q, out, k_new, v_new, workspace):
+        assert t is None or t.is_contiguous()
+    nq = q.shape[3]
+    assert q.shape == out.shape and q.dtype == out.dtype and q.shape[0] == S and q.shape[1] == qc.L \
+        and q.shape[4] == qc.D
+    for t in (k_new, v_new):
+        assert t is None or (t.dtype == q.dtype and tuple(t.shape) == (S, qc.L, qc.Hkv, nq, qc.D))
+    rc = lib.kvr_quant_attn(ctypes.byref(qc), _ints(ctx_len, qc.S), ctypes.byref(oc) if oc else None,
+                            _ints(len_, S), _ptr(q), dtype_code(q.dtype), q.shape[2], nq, float(scale), _ptr(k_new),
+                            _ptr(v_new), _ints(new_pos, S * nq), _ptr(out), _ptr(workspace),
+                            0 if workspace is None else workspace.numel() * workspace.element_size(),
+                            _stream(stream))
+    _check(rc, "kvr_quant_attn")
+
+
+def verify_draft_workspace_size(S: int, T: int, V: int, Vd: int, top_k: int) -> int:
+    return int(lib.kvr_verify_draft_workspace_size(S, T, V, Vd, top_k))
+
+
+def verify_draft(logits: torch.Tensor, draft_tokens: torch.Tensor, sampler: Sampler, u_accept: torch.Tensor,
+                 u_draw: torch.Tensor, accepted: torch.Tensor, tokens: torch.Tensor,
+                 draft_logits: Optional[torch.Tensor] = None, V: Optional[int] = None, Vd: Optional[int] = None,
+                 n_draft: Optional[torch.Tensor] = None, draft_sampler: Optional[Sampler] = None,
+                 len_: Optional[torch.Tensor] = None, len_out: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """kvr_verify_draft: logits[S * (T + 1)][ld] and draft_logits[S * T][ldd] (None: looked-up tokens) over
+    draft_tokens[S][T]; accepted[S], tokens[S][T + 1] and, with len_, len_out[S] are written."""
+    S, T = draft_tokens.shape
+    assert logits.dim() == 2 and logits.stride(1) == 1 and logits.shape[0] == S * (T + 1)
+    if draft_logits is not None:
+        assert draft_logits.dim() == 2 and draft_logits.stride(1) == 1 and draft_logits.shape[0] == S * T
+        assert draft_logits.dtype == logits.dtype
+        Vd = draft_logits.shape[1] if Vd is None else Vd
+    V = logits.shape[1] if V is None else V
+    for t, n in ((u_accept, S * T), (u_draw, S)):
+        assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n
+    assert workspace is None or workspace.is_contiguous()
+    rc = lib.kvr_verify_draft(_ptr(logits), V, logits.stride(0), _ptr(draft_logits), Vd or 0,
+                              0 if draft_logits is None else draft_logits.stride(0), dtype_code(logits.dtype), S, T,
+                              _ints(draft_tokens, S * T), _ints(n_draft, S), ctypes.byref(sampler.c()),
+                              ctypes.byref(draft_sampler.c()) if draft_sampler is not None else None, _ptr(u_accept),
+                              _ptr(u_draw), _ints(accepted, S), _ints(tokens, S * (T + 1)), _ints(len_, S),
+                              _ints(len_out, S), _ptr(workspace),
+                              0 if workspace is None else workspace.numel() * workspace.element_size(),
+                              _stream(stream))
+    _check(rc, "kvr_verify_draft")
