@@ -219,6 +219,10 @@ struct QuantAttnParams {
   const void *k_new, *v_new;  // [S][L][Hkv][nq][D], or NULL
   const int32_t *new_pos;     // [S][nq], or NULL
   float *ws;
+  // Plan of a bfloat16 call: row blocks per wave and groups of them, waves of
+  // the context kernel and their least span in tiles, rows per workgroup of
+  // the join.
+  int rb, row_groups, nwaves, min_span, rpw;
 };
 size_t quant_attn_workspace_bytes(const QuantAttnParams &p);
 hipError_t launch_quant_attn(const QuantAttnParams &p, hipStream_t stream);

@@ -192,30 +192,808 @@ __global__ __launch_bounds__(kThreads) void quant_attn_vector(QuantAttnParams p)
     }
 }
 
-template <typename T, int D, int NG>
-void launch_vector(const QuantAttnParams &p, hipStream_t stream) {
-  const dim3 grid((uint32_t)p.S * p.L * p.Hkv * p.nq);
-  hipLaunchKernelGGL((quant_attn_vector<T, D, NG>), grid, dim3(kThreads), 0, stream, p);
+
+// ---------------------------------------------------------------------------
+// bfloat16: matrix products straight from the codes.
+//
+// A unit (context, layer, KV head) has R = C nq G query rows, in blocks of 16.
+// With k_j = z + s n (per group) the logit of a key is
+//   q.k = sum_groups s (q.n) + z (sum of q in the group),
+// and the output of column d is
+//   sum_j p_j v_jd = sum_j (p_j s_j) n_jd + sum_j p_j z_j,
+// so the codes themselves are matrix operands, and scales and offsets touch
+// one number per key and group. A code placed in the low bits of a float16 is
+// the subnormal n 2^-24 (or n 2^-20 four bits up), which the matrix cores take
+// as exactly that; expanding eight codes costs one shift and four ands.
+//   S^T = K.Q^T : A = codes of 16 keys x 32 d, B = q in float16, per row scaled
+//     by a power of two so that bfloat16's values stay exact (2^-25 of the
+//     row's largest). A product per group, then an fma by the keys' scales.
+//     The offsets' part is one more product over the groups' sums of q, held
+//     as three float16 terms.
+//   O = P.V : P is float16 (the layout of S^T is the A operand's), P s its
+//     product with the scales of a group, B = codes. One more product has the
+//     offsets as columns and a column of ones: the sums of p, as rounded.
+// Rounding p and p s to float16 costs 2^-11 each, below the bfloat16 output's
+// 2^-8; sums stay in float32.
+//
+// Work: the tiles of all units, one after the other, are cut into equal spans,
+// one wave each, as many as the chip holds at once; a wave leaves one partial
+// record per unit that its span touches. The lengths are read on the device,
+// so the cut follows them. A second kernel joins the records with the
+// sequence's own rows.
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+
+__device__ __forceinline__ rsrc_t make_rsrc(const void *p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)0, (int)bytes, 0x00020000);
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((float2_t){a, b}, half2_t));
+}
+__device__ __forceinline__ uint32_t mul_f16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, a) * __builtin_bit_cast(half2_t, b));
+}
+__device__ __forceinline__ float4_t mfma_f16(u32x4 a, u32x4 b, float4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float4_t mfma_f16_k16(u32x2 a, u32x2 b, float4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(half4_t, a), __builtin_bit_cast(half4_t, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float4_t mfma_bf16(u32x4 a, u32x4 b, float4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+// Lane 0's value as a scalar.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// A partial record of one query row: (max, sum, -, -) in the log2 domain, then
+// o / sum as D float16.
+template <int D>
+constexpr int kRecFloats = 4 + D / 2;
+
+// The running reference of a row's exponents may trail its largest by this
+// much (log2): p stays below 16, p s below float16's largest (s <= 2184.6).
+constexpr float kSlack = 4.0f;
+constexpr float kUnset = -3.0e38f;
+
+// How the tiles are cut: waves of `span` tiles over all units in order.
+struct Cut {
+  long span;
+  long total;
+};
+
+__device__ __forceinline__ int ctx_tiles(const QuantAttnParams &p, int c) {
+  return c < p.P ? (ctx_len(p, c) + kQuantTile - 1) / kQuantTile : 0;
 }
 
-template <typename T>
-void launch_type(const QuantAttnParams &p, hipStream_t stream) {
-  if (p.D == 128) {
-    if (p.group == 32) launch_vector<T, 128, 4>(p, stream);
-    else launch_vector<T, 128, 2>(p, stream);
+// Tiles of the contexts before c0 .. c0 + 63, inclusive scan over the lanes.
+__device__ __forceinline__ int scan_tiles(int t, int lane) {
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int o = __shfl_up(t, off, kWave);
+    if (lane >= off) t += o;
+  }
+  return t;
+}
+
+__device__ __forceinline__ Cut cut_of(const QuantAttnParams &p, int lane) {
+  long sum = 0;
+  for (int c0 = 0; c0 < p.P; c0 += kWave) {
+    int t = ctx_tiles(p, c0 + lane);
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) t += shfl_xor(t, m);
+    sum += t;
+  }
+  Cut cut;
+  cut.total = sum * p.L * p.Hkv;
+  cut.span = max((cut.total + p.nwaves - 1) / p.nwaves, (long)p.min_span);
+  return cut;
+}
+
+// Data of one tile as a lane holds it.
+template <int D, int NG>
+struct Chunk {
+  u32x4 k[D / 64], v[D / 64];
+  uint32_t ks[2][2 * NG];  // scales of keys 16 t + 4 g + 0..3: [key][group] float16
+  uint32_t kz[2];          // offset of key 16 t + n in group g
+  u32x4 vs[NG];            // scales of the lane's 8 slots
+  u32x4 vz;                // column n: offsets of group n
+};
+
+// Constant byte offsets of a lane's loads within a tile.
+template <int D, int NG>
+struct Offsets {
+  uint32_t code, ks, kz, vs, vz;
+  __device__ __forceinline__ explicit Offsets(int lane) {
+    const int n = lane & 15, g = lane >> 4;
+    code = lane * 16;
+    ks = g * 8 * NG;
+    kz = g < NG ? (n * NG + g) * 2 : 0x40000000u;  // past the resource: zero
+    vs = g * 16;
+    vz = n < NG ? n * 64 + g * 16 : 0x40000000u;
+  }
+};
+
+template <int D, int NG>
+__device__ __forceinline__ void load_tile(Chunk<D, NG> &c, const char *tile, bool live, const Offsets<D, NG> &o) {
+  using Q = QTile<D, NG>;
+  const rsrc_t r = make_rsrc(tile, live ? Q::BYTES : 0);
+#pragma unroll
+  for (int i = 0; i < D / 64; i++) c.k[i] = __builtin_amdgcn_raw_buffer_load_b128(r, o.code + i * 1024, 0, kStreamLoad);
+#pragma unroll
+  for (int i = 0; i < D / 64; i++)
+    c.v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, o.code + i * 1024, Q::VC, kStreamLoad);
+#pragma unroll
+  for (int t = 0; t < 2; t++) {
+    if constexpr (NG == 4) {
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, o.ks + t * 128 + h * 16, Q::KS, kStreamLoad);
+#pragma unroll
+        for (int i = 0; i < 4; i++) c.ks[t][4 * h + i] = x[i];
+      }
+    } else if constexpr (NG == 2) {
+      const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, o.ks + t * 64, Q::KS, kStreamLoad);
+#pragma unroll
+      for (int i = 0; i < 4; i++) c.ks[t][i] = x[i];
+    } else {
+      const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, o.ks + t * 32, Q::KS, kStreamLoad);
+      c.ks[t][0] = x[0];
+      c.ks[t][1] = x[1];
+    }
+    c.kz[t] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, o.kz + t * 32 * NG, Q::KZ, kStreamLoad);
+  }
+#pragma unroll
+  for (int i = 0; i < NG; i++) c.vs[i] = __builtin_amdgcn_raw_buffer_load_b128(r, o.vs + i * 64, Q::VS, kStreamLoad);
+  c.vz = __builtin_amdgcn_raw_buffer_load_b128(r, o.vz, Q::VZ, kStreamLoad);
+}
+
+// The query operands of one row block and what is summed for it.
+template <int D, int NG>
+struct Block {
+  u32x4 q[D / 32];      // B operand of step i
+  u32x2 qz;             // B operand of the offsets' product
+  float c1, c2;         // logits (log2) = c1 codes' part + c2 offsets' part
+  int limit;            // visible keys of the lane's row
+  float ref;            // exponents' reference of the lane's row
+  float4_t o[D / 16];   // rows 4 g + 0..3, column n of instance b
+  float4_t z;           // the same rows; column: group's offsets, NG: sum of p
+};
+
+// Four code operands of a code word: codes 0 and 4 (times 2^-24), 1 and 5 (times 2^-20), 2 and 6, 3 and 7.
+__device__ __forceinline__ u32x4 expand(uint32_t w) {
+  const uint32_t h = w >> 8;
+  return (u32x4){w & 0x000f000fu, w & 0x00f000f0u, h & 0x000f000fu, h & 0x00f000f0u};
+}
+
+template <int D, int NG>
+__device__ __forceinline__ void load_queries(Block<D, NG> &b, const QuantAttnParams &p, const bf16_t *row, int lane) {
+  const int g = lane >> 4;
+  float x[D / 32][8];
+  float big = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; i++) {
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if (row) w = *reinterpret_cast<const u32x4 *>(row + 32 * i + 8 * g);
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      x[i][2 * e] = bf16_lo(w[e]);
+      x[i][2 * e + 1] = bf16_hi(w[e]);
+      big = fmaxf(big, fmaxf(fabsf(x[i][2 * e]), fabsf(x[i][2 * e + 1])));
+    }
+  }
+  big = fmaxf(big, shfl_xor(big, 16));
+  big = fmaxf(big, shfl_xor(big, 32));
+  // The row times 2^-e lies in [2^8, 2^9) at its largest.
+  int e = 0;
+  if (big > 0.f && big < __builtin_huge_valf()) e = ilogbf(big) - 8;
+  float sum[NG];
+#pragma unroll
+  for (int k = 0; k < NG; k++) sum[k] = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; i++) {
+#pragma unroll
+    for (int k = 0; k < 8; k++) {
+      x[i][k] = ldexpf(x[i][k], -e);
+      sum[i * NG / (D / 32)] += x[i][k];
+    }
+    b.q[i][0] = pack_f16(x[i][0], x[i][4]);
+    b.q[i][1] = pack_f16(x[i][1] * 0.0625f, x[i][5] * 0.0625f);
+    b.q[i][2] = pack_f16(x[i][2], x[i][6]);
+    b.q[i][3] = pack_f16(x[i][3] * 0.0625f, x[i][7] * 0.0625f);
+  }
+  float mine = 0.f;  // the sum of group g
+#pragma unroll
+  for (int k = 0; k < NG; k++) {
+    sum[k] += shfl_xor(sum[k], 16);
+    sum[k] += shfl_xor(sum[k], 32);
+    mine = k == g ? sum[k] : mine;
+  }
+  const float hi = (float)(f16_t)mine, mid = (float)(f16_t)(mine - hi);
+  b.qz[0] = pack_f16(hi, mid);
+  b.qz[1] = pack_f16(mine - hi - mid, 0.f);
+  b.c2 = ldexpf(p.scale * kLog2e, e);
+  b.c1 = ldexpf(p.scale * kLog2e, e + 24);
+}
+
+template <int D, int NG>
+__device__ __forceinline__ void clear(Block<D, NG> &b) {
+  b.ref = kUnset;
+#pragma unroll
+  for (int i = 0; i < D / 16; i++) b.o[i] = (float4_t){0.f, 0.f, 0.f, 0.f};
+  b.z = (float4_t){0.f, 0.f, 0.f, 0.f};
+}
+
+// One tile for RB row blocks; key0: the tile's first key; tail: some row does
+// not see some of its keys, or it has slots past the context's last.
+template <int D, int NG, int RB>
+__device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], Chunk<D, NG> &c, int key0, int n_ctx, bool tail,
+                                          int lane) {
+  const int n = lane & 15, g = lane >> 4;
+  if (tail) {
+    // Slots past the last hold anything: their scales and offsets become 0.
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const int k0 = key0 + (r < 2 ? 4 * g + 2 * r : 16 + 4 * g + 2 * (r - 2));
+      const uint32_t m = (k0 < n_ctx ? 0xffffu : 0u) | (k0 + 1 < n_ctx ? 0xffff0000u : 0u);
+#pragma unroll
+      for (int i = 0; i < NG; i++) c.vs[i][r] &= m;
+      c.vz[r] &= m;
+    }
+  }
+  u32x4 vz = c.vz;
+#pragma unroll
+  for (int r = 0; r < 4; r++) vz[r] = n == NG ? 0x3c003c00u : vz[r];  // the column of ones
+  u32x4 p[RB];
+  {
+    u32x4 ka[2][D / 32];
+    u32x2 kz[2];
+#pragma unroll
+    for (int t = 0; t < 2; t++) {
+#pragma unroll
+      for (int i = 0; i < D / 32; i++) ka[t][i] = expand(D == 128 ? c.k[t * (D / 64) / 2][i] : c.k[0][2 * t + i]);
+      kz[t] = (u32x2){c.kz[t] | (c.kz[t] << 16), c.kz[t]};
+    }
+#pragma unroll
+    for (int b = 0; b < RB; b++) {
+      Block<D, NG> &B = blk[b];
+      float xs[2][4], xz[2][4], d[2][4];
+#pragma unroll
+      for (int t = 0; t < 2; t++) {
+        const float4_t zt = mfma_f16_k16(kz[t], B.qz, (float4_t){0.f, 0.f, 0.f, 0.f});
+        constexpr int PER = D / 32 / NG;  // products per group
+#pragma unroll
+        for (int k = 0; k < NG; k++) {
+          float4_t a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < PER; i++) a = mfma_f16(ka[t][k * PER + i], B.q[k * PER + i], a);
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            const int at = j * NG + k;
+            const half2_t h = __builtin_bit_cast(half2_t, c.ks[t][at >> 1]);
+            const float sc = (float)h[at & 1];
+            xs[t][j] = k == 0 ? a[j] * sc : fmaf(a[j], sc, xs[t][j]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          xz[t][j] = zt[j];
+          d[t][j] = fmaf(xs[t][j], B.c1, fmaf(zt[j], B.c2, -B.ref));
+        }
+        if (tail) {
+#pragma unroll
+          for (int j = 0; j < 4; j++) d[t][j] = key0 + 16 * t + 4 * g + j < B.limit ? d[t][j] : kNegInf;
+        }
+      }
+      float top = fmaxf(fmaxf(fmaxf(d[0][0], d[0][1]), fmaxf(d[0][2], d[0][3])),
+                        fmaxf(fmaxf(d[1][0], d[1][1]), fmaxf(d[1][2], d[1][3])));
+      if (__any(top > kSlack)) {
+        // A new reference for the rows that need one: their largest logit so far.
+        float m = kNegInf;
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            float x = fmaf(xs[t][j], B.c1, xz[t][j] * B.c2);
+            if (tail) x = key0 + 16 * t + 4 * g + j < B.limit ? x : kNegInf;
+            m = fmaxf(m, x);
+          }
+        m = fmaxf(m, shfl_xor(m, 16));
+        m = fmaxf(m, shfl_xor(m, 32));
+        const float ref = fmaxf(B.ref, m);
+        const float f = fast_exp2(B.ref - ref);
+        B.ref = ref;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const float fj = __shfl(f, 4 * g + j, kWave);
+#pragma unroll
+          for (int i = 0; i < D / 16; i++) B.o[i][j] *= fj;
+          B.z[j] *= fj;
+        }
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            d[t][j] = fmaf(xs[t][j], B.c1, fmaf(xz[t][j], B.c2, -ref));
+            if (tail) d[t][j] = key0 + 16 * t + 4 * g + j < B.limit ? d[t][j] : kNegInf;
+          }
+      }
+      float e[2][4];
+#pragma unroll
+      for (int t = 0; t < 2; t++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) e[t][j] = fast_exp2(d[t][j]);
+      p[b] = (u32x4){pack_f16(e[0][0], e[0][1]), pack_f16(e[0][2], e[0][3]), pack_f16(e[1][0], e[1][1]),
+                     pack_f16(e[1][2], e[1][3])};
+      B.z = mfma_f16(p[b], vz, B.z);
+    }
+  }
+  // Values: half h of the codes has instances 4 h .. 4 h + 3, groups of 2 or 4 instances.
+#pragma unroll
+  for (int h = 0; h < D / 64; h++) {
+    u32x4 vb[4];
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const u32x4 x = expand(c.v[h][r]);
+#pragma unroll
+      for (int i = 0; i < 4; i++) vb[i][r] = x[i];
+    }
+#pragma unroll
+    for (int b = 0; b < RB; b++) {
+      constexpr int IPG = QTile<D, NG>::GROUP / 16;  // instances per group
+      u32x4 ps;
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const int inst = 4 * h + i;
+        if (inst % IPG == 0 || i == 0) {
+#pragma unroll
+          for (int r = 0; r < 4; r++) ps[r] = mul_f16(p[b][r], c.vs[inst / IPG][r]);
+        }
+        blk[b].o[inst] = mfma_f16(ps, vb[i], blk[b].o[inst]);
+      }
+    }
+  }
+}
+
+// Context kernel: one wave per span.
+template <int D, int NG, int RB>
+__global__ __launch_bounds__(kWave) void quant_ctx(QuantAttnParams p) {
+  using Q = QTile<D, NG>;
+  const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
+  // The row groups of a span run eight workgroups apart, on one XCD.
+  const int xcd = blockIdx.x & 7, k8 = blockIdx.x >> 3;
+  const int w = (k8 / p.row_groups) * 8 + xcd, rg = k8 % p.row_groups;
+  if (w >= p.nwaves) return;
+  const Cut cut = cut_of(p, lane);
+  const long pos0 = w * cut.span, end = min(pos0 + cut.span, cut.total);
+  if (pos0 >= end) return;
+  const int lh = p.L * p.Hkv, rows = p.C * p.nq * p.G, per = p.nq * p.G;
+  // The context that holds pos0.
+  int c = 0;
+  long at = 0;  // tiles before context c
+  for (int c0 = 0; c0 < p.P; c0 += kWave) {
+    const int t = ctx_tiles(p, c0 + lane), sc = scan_tiles(t, lane);
+    const uint64_t past = __ballot((at + sc) * lh > pos0);
+    if (past) {
+      const int i = __ffsll((long long)past) - 1;
+      c = c0 + i;
+      at += __shfl(sc - t, i, kWave);
+      break;
+    }
+    at += __shfl(sc, kWave - 1, kWave);
+  }
+  long pos = pos0;
+  int n_ctx = uniform(ctx_len(p, c)), tiles = (n_ctx + kQuantTile - 1) / kQuantTile;
+  int u = uniform((int)((pos - at * lh) / tiles));       // unit within the context
+  int tile = uniform((int)((pos - at * lh) % tiles));
+  const Offsets<D, NG> off(lane);
+  Block<D, NG> blk[RB];
+  while (pos < end) {
+    const int last = (int)min((long)tiles, tile + (end - pos));
+    const int l = u / p.Hkv, h = u % p.Hkv;
+    const char *base = static_cast<const char *>(p.data) + ((size_t)c * lh + u) * p.ntiles * Q::BYTES;
+    Chunk<D, NG> a, b;
+    load_tile<D, NG>(a, base + (size_t)tile * Q::BYTES, true, off);
+    int least = n_ctx;
+#pragma unroll
+    for (int i = 0; i < RB; i++) {
+      const int r = (rg * RB + i) * 16 + n;
+      const bf16_t *row = nullptr;
+      blk[i].limit = n_ctx;
+      if (r < rows) {
+        const int s = c * p.C + r / per, rr = r % per;
+        row = static_cast<const bf16_t *>(p.q) + ((((size_t)s * p.L + l) * p.Hkv + h) * per + rr) * D;
+        blk[i].limit = (int)min((long)n_ctx, (long)n_ctx + own_len(p, s) - (p.nq - 1 - rr % p.nq));
+      }
+      load_queries<D, NG>(blk[i], p, row, lane);
+      clear<D, NG>(blk[i]);
+      int m = blk[i].limit;
+#pragma unroll
+      for (int x = 8; x >= 1; x >>= 1) m = min(m, shfl_xor(m, x));
+      least = min(least, uniform(m));
+    }
+    for (int t = tile; t < last; t += 2) {
+      load_tile<D, NG>(b, base + (size_t)(t + 1) * Q::BYTES, t + 1 < last, off);
+      tile_step<D, NG, RB>(blk, a, t * Q::KEYS, n_ctx, (t + 1) * Q::KEYS > least, lane);
+      if (t + 1 >= last) break;
+      load_tile<D, NG>(a, base + (size_t)(t + 2) * Q::BYTES, t + 2 < last, off);
+      tile_step<D, NG, RB>(blk, b, (t + 1) * Q::KEYS, n_ctx, (t + 2) * Q::KEYS > least, lane);
+    }
+    // The records of this piece.
+    float *rec = p.ws + ((size_t)w + (size_t)c * lh + u) * rows * kRecFloats<D>;
+#pragma unroll
+    for (int i = 0; i < RB; i++) {
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const int r = (rg * RB + i) * 16 + 4 * g + j;
+        const float den = __shfl(blk[i].z[j], (lane & 48) + NG, kWave);
+        const float ref = __shfl(blk[i].ref, 4 * g + j, kWave);
+        const float inv = den > 0.f ? 1.0f / den : 0.f;
+        float off_j[NG];
+#pragma unroll
+        for (int k = 0; k < NG; k++) off_j[k] = __shfl(blk[i].z[j], (lane & 48) + k, kWave);
+        if (r < rows) {
+          float *to = rec + (size_t)r * kRecFloats<D>;
+          if (n == 0) *reinterpret_cast<float2_t *>(to) = (float2_t){den > 0.f || den != den ? ref : kNegInf, den};
+#pragma unroll
+          for (int x = 0; x < D / 32; x++) {
+            const float o = off_j[x * 32 / Q::GROUP];
+            reinterpret_cast<uint32_t *>(to + 4)[x * 16 + n] =
+                pack_f16((blk[i].o[2 * x][j] * 0x1p24f + o) * inv, (blk[i].o[2 * x + 1][j] * 0x1p20f + o) * inv);
+          }
+        }
+      }
+    }
+    pos += last - tile;
+    tile = 0;
+    if (++u == lh && pos < end) {
+      u = 0;
+      do {
+        c++;
+        n_ctx = uniform(ctx_len(p, c));
+      } while (n_ctx == 0);  // pos < end: a later context has tiles
+      tiles = (n_ctx + kQuantTile - 1) / kQuantTile;
+    }
+  }
+}
+
+// One chunk of 32 own keys as a lane holds it: the rows of K as the A operand
+// (keys n and 16 + n, d = 32 i + 8 g + 0..7), of V the 8 keys of the lane's
+// slots at d = n D / 16 ...
+template <int D>
+struct OwnChunk {
+  u32x4 k[2][D / 32];
+  uint32_t v[8][D / 32];
+};
+
+template <int D>
+__device__ __forceinline__ int slot_key(int g, int e) { return e < 4 ? 4 * g + e : 16 + 4 * g + e - 4; }
+
+template <int D>
+__device__ __forceinline__ void load_own(OwnChunk<D> &c, const OwnRows<bf16_t> &K, const OwnRows<bf16_t> &V, int key0, int u,
+                                         int lane) {
+  const int n = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int t = 0; t < 2; t++) {
+    const bf16_t *row = K.row(min(key0 + 16 * t + n, u - 1), D);
+#pragma unroll
+    for (int i = 0; i < D / 32; i++) c.k[t][i] = *reinterpret_cast<const u32x4 *>(row + 32 * i + 8 * g);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; e++) {
+    const bf16_t *row = V.row(min(key0 + slot_key<D>(g, e), u - 1), D) + n * (D / 16);
+    if constexpr (D == 128) {
+      const u32x4 x = *reinterpret_cast<const u32x4 *>(row);
+#pragma unroll
+      for (int i = 0; i < 4; i++) c.v[e][i] = x[i];
+    } else {
+      const u32x2 x = *reinterpret_cast<const u32x2 *>(row);
+      c.v[e][0] = x[0];
+      c.v[e][1] = x[1];
+    }
+  }
+}
+
+constexpr int kOwnWaves = 4;
+
+// Second kernel: one workgroup per (sequence, layer, KV head) and rpw of its
+// rows. Its waves attend to the own rows (32 keys at a time, in turn), with p
+// as two bfloat16 terms; then all of them join these and the context's
+// records: 16 lanes per row, the records of a row dealt to 16 / rpw groups.
+template <int D, int NG>
+__global__ __launch_bounds__(kOwnWaves *kWave) void quant_join(QuantAttnParams p) {
+  constexpr int NT = kOwnWaves * kWave, EL = D / 16;  // elements per thread of the join
+  __shared__ float so[kOwnWaves][16][D];
+  __shared__ float sm[16][2];
+  __shared__ float wm[kOwnWaves][16], wl[kOwnWaves][16];
+  const int per = p.nq * p.G, blocks = (per + p.rpw - 1) / p.rpw;
+  const int unit = blockIdx.x / blocks, r0 = blockIdx.x % blocks * p.rpw;
+  const int lh = p.L * p.Hkv, s = unit / lh, c = s / p.C;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, n = lane & 15, g = lane >> 4;
+  const int u = uniform(own_len(p, s));
+  const int nrow = min(p.rpw, per - r0);
+  if (p.ok && r0 == 0) store_new<bf16_t, D, NT>(p, unit, s, u);
+
+  const Cut cut = cut_of(p, lane);
+  // Tiles before this context.
+  long before = 0;
+  for (int c0 = 0; c0 < c; c0 += kWave) {
+    int t = c0 + lane < c ? ctx_tiles(p, c0 + lane) : 0;
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) t += shfl_xor(t, m);
+    before += t;
+  }
+  const int mine = ctx_tiles(p, c);
+
+  if (u > 0) {
+    const size_t own0 = (size_t)unit * p.ocap * D, new0 = (size_t)unit * p.nq * D;
+    const bf16_t *fk = static_cast<const bf16_t *>(p.k_new), *fv = static_cast<const bf16_t *>(p.v_new);
+    const OwnRows<bf16_t> K{static_cast<const bf16_t *>(p.ok) + own0, fk ? fk + new0 : nullptr, u - p.nq};
+    const OwnRows<bf16_t> V{static_cast<const bf16_t *>(p.ov) + own0, fv ? fv + new0 : nullptr, u - p.nq};
+    u32x4 q[D / 32];
+    const bf16_t *row = static_cast<const bf16_t *>(p.q) + ((size_t)unit * per + r0 + min(n, nrow - 1)) * D;
+#pragma unroll
+    for (int i = 0; i < D / 32; i++) q[i] = *reinterpret_cast<const u32x4 *>(row + 32 * i + 8 * g);
+    const int limit = u - (p.nq - 1 - (r0 + min(n, nrow - 1)) % p.nq);  // of the lane's row
+    const float sl2 = p.scale * kLog2e;
+    float m = kNegInf, den = 0.f;
+    float4_t o[D / 16];
+#pragma unroll
+    for (int b = 0; b < D / 16; b++) o[b] = (float4_t){0.f, 0.f, 0.f, 0.f};
+    for (int key0 = wave * 32; key0 < u; key0 += kOwnWaves * 32) {
+      OwnChunk<D> ch;
+      load_own<D>(ch, K, V, key0, u, lane);
+      float x[2][4], top = kNegInf;
+#pragma unroll
+      for (int t = 0; t < 2; t++) {
+        float4_t a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < D / 32; i++) a = mfma_bf16(ch.k[t][i], q[i], a);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          x[t][j] = key0 + 16 * t + 4 * g + j < limit ? a[j] * sl2 : kNegInf;
+          top = fmaxf(top, x[t][j]);
+        }
+      }
+      top = fmaxf(top, shfl_xor(top, 16));
+      top = fmaxf(top, shfl_xor(top, 32));
+      const float mn = fmaxf(m, top), ref = mn == kNegInf ? 0.f : mn;
+      const float f = fast_exp2(m - ref);
+      m = mn;
+      den *= f;
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const float fj = __shfl(f, 4 * g + j, kWave);
+#pragma unroll
+        for (int b = 0; b < D / 16; b++) o[b][j] *= fj;
+      }
+      u32x4 hi, lo;
+#pragma unroll
+      for (int t = 0; t < 2; t++)
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const float e0 = fast_exp2(x[t][j] - ref), e1 = fast_exp2(x[t][j + 1] - ref);
+          den += e0 + e1;
+          const uint32_t w = pack_bf16x2(e0, e1);
+          hi[2 * t + j / 2] = w;
+          lo[2 * t + j / 2] = pack_bf16x2(e0 - bf16_lo(w), e1 - bf16_hi(w));
+        }
+      // Rows past the last live one hold anything; so may rows that only later
+      // queries see, where a value that is not finite would reach the others
+      // as 0 times it: those get a product per query token.
+      const int sees_all = u - (p.nq - 1);
+      bool split = false;
+      if (key0 + 32 > sees_all) {
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          const int key = key0 + slot_key<D>(g, e);
+#pragma unroll
+          for (int i = 0; i < D / 32; i++) {
+            if (key >= u) ch.v[e][i] = 0u;
+            const uint32_t w = ch.v[e][i];
+            odd |= key >= sees_all && ((w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u);
+          }
+        }
+        split = __any(odd);
+      }
+      auto product = [&](const uint32_t (&v)[8][D / 32], float4_t (&acc)[D / 16]) {
+#pragma unroll
+        for (int b = 0; b < D / 16; b++) {
+          u32x4 w;
+#pragma unroll
+          for (int r = 0; r < 4; r++)
+            w[r] = __builtin_amdgcn_perm(v[2 * r + 1][b / 2], v[2 * r][b / 2], b & 1 ? 0x07060302u : 0x05040100u);
+          acc[b] = mfma_bf16(hi, w, acc[b]);
+          acc[b] = mfma_bf16(lo, w, acc[b]);
+        }
+      };
+      if (!split) {
+        product(ch.v, o);
+      } else {
+        for (int t = 0; t < p.nq; t++) {
+          const int lim = u - (p.nq - 1 - t);
+          uint32_t v[8][D / 32];
+          float4_t acc[D / 16];
+#pragma unroll
+          for (int e = 0; e < 8; e++)
+#pragma unroll
+            for (int i = 0; i < D / 32; i++) v[e][i] = key0 + slot_key<D>(g, e) < lim ? ch.v[e][i] : 0u;
+#pragma unroll
+          for (int b = 0; b < D / 16; b++) acc[b] = o[b];
+          product(v, acc);
+#pragma unroll
+          for (int j = 0; j < 4; j++)
+            if ((r0 + 4 * g + j) % p.nq == t) {
+#pragma unroll
+              for (int b = 0; b < D / 16; b++) o[b][j] = acc[b][j];
+            }
+        }
+      }
+    }
+    den += shfl_xor(den, 16);
+    den += shfl_xor(den, 32);
+    if (g == 0) {
+      wm[wave][n] = m;
+      wl[wave][n] = den;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+#pragma unroll
+      for (int b = 0; b < D / 16; b += 4)
+        *reinterpret_cast<float4_t *>(&so[wave][4 * g + j][n * EL + b]) =
+            (float4_t){o[b][j], o[b + 1][j], o[b + 2][j], o[b + 3][j]};
+  }
+  __syncthreads();
+
+  // Join. Thread: row r0 + slot % rpw, records part, part + parts, .. of it, elements sub * EL ..
+  const int slot = tid / 16, sub = tid % 16, parts = 16 / p.rpw;
+  const int row = slot % p.rpw, part = slot / p.rpw;
+  float m = kNegInf, den = 0.f, o[EL];
+#pragma unroll
+  for (int e = 0; e < EL; e++) o[e] = 0.f;
+  auto fold = [&](float mr, float lr, float scale, const float (&x)[EL]) {
+    // lr: weight of the record's sum; scale: of its (unnormalised) values.
+    if (lr == 0.f) return;
+    const float mn = fmaxf(m, mr);
+    const float fa = m == kNegInf ? 0.f : fast_exp2(m - mn), fb = fast_exp2(mr - mn);
+    m = mn;
+    den = den * fa + lr * fb;
+    const float sb = scale * fb;
+#pragma unroll
+    for (int e = 0; e < EL; e++) o[e] = fmaf(x[e], sb, o[e] * fa);
+  };
+  if (row < nrow) {
+    if (part == 0 && u > 0) {
+#pragma unroll
+      for (int w = 0; w < kOwnWaves; w++) {
+        float x[EL];
+#pragma unroll
+        for (int e = 0; e < EL; e++) x[e] = so[w][row][sub * EL + e];
+        fold(wm[w][row], wl[w][row], 1.f, x);
+      }
+    }
+    if (mine > 0) {
+      const long first = (before * lh + (long)(unit % lh) * mine), w0 = first / cut.span,
+                 w1 = (first + mine - 1) / cut.span;
+      const int rows = p.C * per, r = s % p.C * per + r0 + row;
+      const size_t cu = (size_t)c * lh + unit % lh;
+      for (long w = w0 + part; w <= w1; w += parts) {
+        const float *rec = p.ws + ((size_t)w + cu) * rows * kRecFloats<D> + (size_t)r * kRecFloats<D>;
+        const float2_t ml = *reinterpret_cast<const float2_t *>(rec);
+        float x[EL];
+        const f16_t *h = reinterpret_cast<const f16_t *>(rec + 4) + sub * EL;
+#pragma unroll
+        for (int e = 0; e < EL; e++) x[e] = (float)h[e];
+        fold(ml[0], ml[1], ml[1], x);
+      }
+    }
+  }
+  if (parts > 1) {
+    __syncthreads();
+    float *po = &so[0][0][0];
+#pragma unroll
+    for (int e = 0; e < EL; e++) po[slot * D + sub * EL + e] = o[e];
+    if (sub == 0) {
+      sm[slot][0] = m;
+      sm[slot][1] = den;
+    }
+    __syncthreads();
+    if (part == 0) {
+      for (int k = 1; k < parts; k++) {
+        float x[EL];
+        const int from = k * p.rpw + row;
+#pragma unroll
+        for (int e = 0; e < EL; e++) x[e] = po[from * D + sub * EL + e];
+        fold(sm[from][0], sm[from][1], 1.f, x);
+      }
+    }
+  }
+  if (part == 0 && row < nrow) {
+    const float inv = den == 0.f ? 0.f : 1.0f / den;
+    uint32_t *to = reinterpret_cast<uint32_t *>(static_cast<bf16_t *>(p.out) + ((size_t)unit * per + r0 + row) * D) +
+                   sub * (EL / 2);
+#pragma unroll
+    for (int e = 0; e < EL; e += 2) to[e / 2] = pack_bf16x2(o[e] * inv, o[e + 1] * inv);
+  }
+}
+
+constexpr int kChipWaves = 2048;  // two waves per SIMD: 256 CUs of four
+constexpr int kMinSpan = 4;
+constexpr int kMaxBlocks = 4;     // row blocks a wave takes at once
+
+// Plan of a bfloat16 call, from shapes alone.
+void plan(QuantAttnParams *p) {
+  const int rows = p->C * p->nq * p->G, blocks = (rows + 15) / 16;
+  p->row_groups = (blocks + kMaxBlocks - 1) / kMaxBlocks;
+  p->rb = (blocks + p->row_groups - 1) / p->row_groups;
+  const double tiles = (double)p->P * p->L * p->Hkv * p->ntiles;
+  const int most = kChipWaves / p->row_groups > 64 ? kChipWaves / p->row_groups : 64;
+  p->min_span = kMinSpan;
+  const double want = tiles / kMinSpan + 1;
+  p->nwaves = want < most ? (int)want : most;
+  // Fewer rows per workgroup of the join where there are few of them.
+  const int per = p->nq * p->G;
+  int rpw = 16;
+  while (rpw > 1 && (long)p->S * p->L * p->Hkv * ((per + rpw - 1) / rpw) < 512) rpw /= 2;
+  p->rpw = rpw;
+}
+
+template <int D, int NG, int RB>
+void launch_ctx(const QuantAttnParams &p, hipStream_t stream) {
+  const uint32_t groups = (uint32_t)(p.nwaves + 7) / 8 * 8 * p.row_groups;
+  hipLaunchKernelGGL((quant_ctx<D, NG, RB>), dim3(groups), dim3(kWave), 0, stream, p);
+}
+
+template <int D, int NG>
+void launch_bf16(const QuantAttnParams &p, hipStream_t stream) {
+  switch (p.rb) {
+    case 1: launch_ctx<D, NG, 1>(p, stream); break;
+    case 2: launch_ctx<D, NG, 2>(p, stream); break;
+    case 3: launch_ctx<D, NG, 3>(p, stream); break;
+    default: launch_ctx<D, NG, 4>(p, stream); break;
+  }
+  const int per = p.nq * p.G;
+  const uint32_t groups = (uint32_t)p.S * p.L * p.Hkv * ((per + p.rpw - 1) / p.rpw);
+  hipLaunchKernelGGL((quant_join<D, NG>), dim3(groups), dim3(kOwnWaves * kWave), 0, stream, p);
+}
+
+template <int D, int NG>
+void launch_any(const QuantAttnParams &p, hipStream_t stream) {
+  if (p.dtype == 0) {
+    const dim3 grid((uint32_t)p.S * p.L * p.Hkv * p.nq);
+    hipLaunchKernelGGL((quant_attn_vector<float, D, NG>), grid, dim3(kThreads), 0, stream, p);
   } else {
-    if (p.group == 32) launch_vector<T, 64, 2>(p, stream);
-    else launch_vector<T, 64, 1>(p, stream);
+    launch_bf16<D, NG>(p, stream);
   }
 }
 
 }  // namespace
 
-size_t quant_attn_workspace_bytes(const QuantAttnParams &) { return 0; }
+size_t quant_attn_workspace_bytes(const QuantAttnParams &params) {
+  if (params.dtype == 0) return 0;
+  QuantAttnParams p = params;
+  plan(&p);
+  // A wave's piece of a unit has record wave + unit.
+  const size_t pieces = (size_t)p.nwaves + (size_t)p.P * p.L * p.Hkv;
+  return pieces * p.C * p.nq * p.G * (4 + p.D / 2) * sizeof(float);
+}
 
-hipError_t launch_quant_attn(const QuantAttnParams &p, hipStream_t stream) {
-  if (p.dtype == 0) launch_type<float>(p, stream);
-  else launch_type<bf16_t>(p, stream);
+hipError_t launch_quant_attn(const QuantAttnParams &params, hipStream_t stream) {
+  QuantAttnParams p = params;
+  plan(&p);
+  if (p.D == 128) {
+    if (p.group == 32) launch_any<128, 4>(p, stream);
+    else launch_any<128, 2>(p, stream);
+  } else {
+    if (p.group == 32) launch_any<64, 2>(p, stream);
+    else launch_any<64, 1>(p, stream);
+  }
   return hipGetLastError();
 }
 
