@@ -250,15 +250,22 @@ __device__ __forceinline__ float4_t mfma_bf16(u32x4 a, u32x4 b, float4_t c) {
 }
 // Lane 0's value as a scalar.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long uniform(long x) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32));
+  return (long)(((uint64_t)hi << 32) | lo);
+}
 
 // A partial record of one query row: (max, sum, -, -) in the log2 domain, then
 // o / sum as D float16.
 template <int D>
 constexpr int kRecFloats = 4 + D / 2;
 
-// The running reference of a row's exponents may trail its largest by this
-// much (log2): p stays below 16, p s below float16's largest (s <= 2184.6).
-constexpr float kSlack = 4.0f;
+// The running reference of a row's exponents is moved where a logit exceeds it
+// by more than kSlack (log2), to kHead below the largest: p stays at most 16,
+// so that p s fits float16 (s <= 2184.6), and is rarely far below 1, where
+// float16 gets coarse. kUnset: no reference yet, any logit sets it.
+constexpr float kSlack = 4.0f, kHead = 3.0f;
 constexpr float kUnset = -3.0e38f;
 
 // How the tiles are cut: waves of `span` tiles over all units in order.
@@ -290,67 +297,39 @@ __device__ __forceinline__ Cut cut_of(const QuantAttnParams &p, int lane) {
     sum += t;
   }
   Cut cut;
-  cut.total = sum * p.L * p.Hkv;
+  cut.total = uniform(sum) * p.L * p.Hkv;
   cut.span = max((cut.total + p.nwaves - 1) / p.nwaves, (long)p.min_span);
   return cut;
 }
 
-// Data of one tile as a lane holds it.
-template <int D, int NG>
-struct Chunk {
-  u32x4 k[D / 64], v[D / 64];
-  uint32_t ks[2][2 * NG];  // scales of keys 16 t + 4 g + 0..3: [key][group] float16
-  uint32_t kz[2];          // offset of key 16 t + n in group g
-  u32x4 vs[NG];            // scales of the lane's 8 slots
-  u32x4 vz;                // column n: offsets of group n
-};
+typedef __attribute__((address_space(3))) void lds_void_t;
 
-// Constant byte offsets of a lane's loads within a tile.
+// s_waitcnt vmcnt(N), other counters unconstrained.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  static_assert(N >= 0 && N < 64, "vmcnt field");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
+// A wave's ring of tiles in LDS. A tile is one block of memory, loaded as it
+// lies by LOADS instructions of 1 KiB (past the end of a unit: zeros, without
+// a memory access); the operands are read from there.
 template <int D, int NG>
-struct Offsets {
-  uint32_t code, ks, kz, vs, vz;
-  __device__ __forceinline__ explicit Offsets(int lane) {
-    const int n = lane & 15, g = lane >> 4;
-    code = lane * 16;
-    ks = g * 8 * NG;
-    kz = g < NG ? (n * NG + g) * 2 : 0x40000000u;  // past the resource: zero
-    vs = g * 16;
-    vz = n < NG ? n * 64 + g * 16 : 0x40000000u;
-  }
+struct Ring {
+  static constexpr int LOADS = (QTile<D, NG>::BYTES + 1023) / 1024;
+  static constexpr int SLOT = LOADS * 1024;
 };
 
 template <int D, int NG>
-__device__ __forceinline__ void load_tile(Chunk<D, NG> &c, const char *tile, bool live, const Offsets<D, NG> &o) {
-  using Q = QTile<D, NG>;
-  const rsrc_t r = make_rsrc(tile, live ? Q::BYTES : 0);
+__device__ __forceinline__ void load_tile(char *slot, const char *tile, bool live, int lane) {
+  const rsrc_t r = make_rsrc(tile, live ? QTile<D, NG>::BYTES : 0);
+#if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
-  for (int i = 0; i < D / 64; i++) c.k[i] = __builtin_amdgcn_raw_buffer_load_b128(r, o.code + i * 1024, 0, kStreamLoad);
-#pragma unroll
-  for (int i = 0; i < D / 64; i++)
-    c.v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, o.code + i * 1024, Q::VC, kStreamLoad);
-#pragma unroll
-  for (int t = 0; t < 2; t++) {
-    if constexpr (NG == 4) {
-#pragma unroll
-      for (int h = 0; h < 2; h++) {
-        const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, o.ks + t * 128 + h * 16, Q::KS, kStreamLoad);
-#pragma unroll
-        for (int i = 0; i < 4; i++) c.ks[t][4 * h + i] = x[i];
-      }
-    } else if constexpr (NG == 2) {
-      const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, o.ks + t * 64, Q::KS, kStreamLoad);
-#pragma unroll
-      for (int i = 0; i < 4; i++) c.ks[t][i] = x[i];
-    } else {
-      const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, o.ks + t * 32, Q::KS, kStreamLoad);
-      c.ks[t][0] = x[0];
-      c.ks[t][1] = x[1];
-    }
-    c.kz[t] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, o.kz + t * 32 * NG, Q::KZ, kStreamLoad);
-  }
-#pragma unroll
-  for (int i = 0; i < NG; i++) c.vs[i] = __builtin_amdgcn_raw_buffer_load_b128(r, o.vs + i * 64, Q::VS, kStreamLoad);
-  c.vz = __builtin_amdgcn_raw_buffer_load_b128(r, o.vz, Q::VZ, kStreamLoad);
+  for (int i = 0; i < Ring<D, NG>::LOADS; i++)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)(slot + i * 1024), 16, lane * 16, i * 1024, 0, kStreamLoad);
+#else
+  (void)r;  // the host pass has no buffer-to-LDS loads
+#endif
 }
 
 // The query operands of one row block and what is summed for it.
@@ -360,7 +339,8 @@ struct Block {
   u32x2 qz;             // B operand of the offsets' product
   float c1, c2;         // logits (log2) = c1 codes' part + c2 offsets' part
   int limit;            // visible keys of the lane's row
-  float ref;            // exponents' reference of the lane's row
+  float nref;           // minus the exponents' reference of the lane's row
+  float above;          // a logit this much above the reference moves it
   float4_t o[D / 16];   // rows 4 g + 0..3, column n of instance b
   float4_t z;           // the same rows; column: group's offsets, NG: sum of p
 };
@@ -423,7 +403,8 @@ __device__ __forceinline__ void load_queries(Block<D, NG> &b, const QuantAttnPar
 
 template <int D, int NG>
 __device__ __forceinline__ void clear(Block<D, NG> &b) {
-  b.ref = kUnset;
+  b.nref = 0.f;
+  b.above = kUnset;
 #pragma unroll
   for (int i = 0; i < D / 16; i++) b.o[i] = (float4_t){0.f, 0.f, 0.f, 0.f};
   b.z = (float4_t){0.f, 0.f, 0.f, 0.f};
@@ -432,127 +413,130 @@ __device__ __forceinline__ void clear(Block<D, NG> &b) {
 // One tile for RB row blocks; key0: the tile's first key; tail: some row does
 // not see some of its keys, or it has slots past the context's last.
 template <int D, int NG, int RB>
-__device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], Chunk<D, NG> &c, int key0, int n_ctx, bool tail,
+__device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *slot, int key0, int n_ctx, bool tail,
                                           int lane) {
+  using Q = QTile<D, NG>;
   const int n = lane & 15, g = lane >> 4;
+  float d[RB][2][4];  // logits less the rows' references (log2)
+#pragma unroll
+  for (int t = 0; t < 2; t++) {
+    constexpr int PER = D / 32 / NG;  // products per group
+    const u32x4 code = *reinterpret_cast<const u32x4 *>(slot + (D == 128 ? t * 1024 : 0) + lane * 16);
+    uint32_t z = *reinterpret_cast<const uint16_t *>(slot + Q::KZ + t * 32 * NG + (n * NG + (NG == 4 ? g : g & (NG - 1))) * 2);
+    if (NG < 4) z = g < NG ? z : 0u;
+    const u32x2 kz = {z | (z << 16), z};
+    uint32_t ks[2 * NG];  // scales of keys 4 g .. 4 g + 3: [key][group] float16
+#pragma unroll
+    for (int i = 0; i < 2 * NG; i++) ks[i] = *reinterpret_cast<const uint32_t *>(slot + Q::KS + t * 32 * NG + g * 8 * NG + i * 4);
+    u32x4 ka[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; i++) ka[i] = expand(code[D == 128 ? i : 2 * t + i]);
+#pragma unroll
+    for (int b = 0; b < RB; b++) {
+      const Block<D, NG> &B = blk[b];
+      const float4_t zt = mfma_f16_k16(kz, B.qz, (float4_t){0.f, 0.f, 0.f, 0.f});
+      float xs[4];
+#pragma unroll
+      for (int k = 0; k < NG; k++) {
+        float4_t a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < PER; i++) a = mfma_f16(ka[k * PER + i], B.q[k * PER + i], a);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const int at = j * NG + k;
+          const half2_t h = __builtin_bit_cast(half2_t, ks[at >> 1]);
+          const float sc = (float)h[at & 1];
+          xs[j] = k == 0 ? a[j] * sc : fmaf(a[j], sc, xs[j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        d[b][t][j] = fmaf(xs[j], B.c1, fmaf(zt[j], B.c2, B.nref));
+      }
+    }
+  }
+  u32x4 vs[NG], vz;
+#pragma unroll
+  for (int i = 0; i < NG; i++) vs[i] = *reinterpret_cast<const u32x4 *>(slot + Q::VS + i * 64 + g * 16);
+  vz = *reinterpret_cast<const u32x4 *>(slot + Q::VZ + (n & (NG - 1)) * 64 + g * 16);
   if (tail) {
+    asm volatile("");  // a branch, not selects in every tile
+#pragma unroll
+    for (int b = 0; b < RB; b++)
+#pragma unroll
+      for (int t = 0; t < 2; t++)
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+          d[b][t][j] = key0 + 16 * t + 4 * g + j < blk[b].limit ? d[b][t][j] : kNegInf;
     // Slots past the last hold anything: their scales and offsets become 0.
 #pragma unroll
     for (int r = 0; r < 4; r++) {
       const int k0 = key0 + (r < 2 ? 4 * g + 2 * r : 16 + 4 * g + 2 * (r - 2));
       const uint32_t m = (k0 < n_ctx ? 0xffffu : 0u) | (k0 + 1 < n_ctx ? 0xffff0000u : 0u);
 #pragma unroll
-      for (int i = 0; i < NG; i++) c.vs[i][r] &= m;
-      c.vz[r] &= m;
+      for (int i = 0; i < NG; i++) vs[i][r] &= m;
+      vz[r] &= m;
     }
   }
-  u32x4 vz = c.vz;
+  // Column NG holds ones; what the columns after it hold is not used.
 #pragma unroll
-  for (int r = 0; r < 4; r++) vz[r] = n == NG ? 0x3c003c00u : vz[r];  // the column of ones
+  for (int r = 0; r < 4; r++) vz[r] = n == NG ? 0x3c003c00u : vz[r];
   u32x4 p[RB];
-  {
-    u32x4 ka[2][D / 32];
-    u32x2 kz[2];
 #pragma unroll
-    for (int t = 0; t < 2; t++) {
+  for (int b = 0; b < RB; b++) {
+    Block<D, NG> &B = blk[b];
+    float top = kNegInf;
 #pragma unroll
-      for (int i = 0; i < D / 32; i++) ka[t][i] = expand(D == 128 ? c.k[t * (D / 64) / 2][i] : c.k[0][2 * t + i]);
-      kz[t] = (u32x2){c.kz[t] | (c.kz[t] << 16), c.kz[t]};
-    }
+    for (int t = 0; t < 2; t++)
 #pragma unroll
-    for (int b = 0; b < RB; b++) {
-      Block<D, NG> &B = blk[b];
-      float xs[2][4], xz[2][4], d[2][4];
-#pragma unroll
-      for (int t = 0; t < 2; t++) {
-        const float4_t zt = mfma_f16_k16(kz[t], B.qz, (float4_t){0.f, 0.f, 0.f, 0.f});
-        constexpr int PER = D / 32 / NG;  // products per group
-#pragma unroll
-        for (int k = 0; k < NG; k++) {
-          float4_t a = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int i = 0; i < PER; i++) a = mfma_f16(ka[t][k * PER + i], B.q[k * PER + i], a);
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            const int at = j * NG + k;
-            const half2_t h = __builtin_bit_cast(half2_t, c.ks[t][at >> 1]);
-            const float sc = (float)h[at & 1];
-            xs[t][j] = k == 0 ? a[j] * sc : fmaf(a[j], sc, xs[t][j]);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          xz[t][j] = zt[j];
-          d[t][j] = fmaf(xs[t][j], B.c1, fmaf(zt[j], B.c2, -B.ref));
-        }
-        if (tail) {
-#pragma unroll
-          for (int j = 0; j < 4; j++) d[t][j] = key0 + 16 * t + 4 * g + j < B.limit ? d[t][j] : kNegInf;
-        }
-      }
-      float top = fmaxf(fmaxf(fmaxf(d[0][0], d[0][1]), fmaxf(d[0][2], d[0][3])),
-                        fmaxf(fmaxf(d[1][0], d[1][1]), fmaxf(d[1][2], d[1][3])));
-      if (__any(top > kSlack)) {
-        // A new reference for the rows that need one: their largest logit so far.
-        float m = kNegInf;
-#pragma unroll
-        for (int t = 0; t < 2; t++)
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            float x = fmaf(xs[t][j], B.c1, xz[t][j] * B.c2);
-            if (tail) x = key0 + 16 * t + 4 * g + j < B.limit ? x : kNegInf;
-            m = fmaxf(m, x);
-          }
-        m = fmaxf(m, shfl_xor(m, 16));
-        m = fmaxf(m, shfl_xor(m, 32));
-        const float ref = fmaxf(B.ref, m);
-        const float f = fast_exp2(B.ref - ref);
-        B.ref = ref;
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          const float fj = __shfl(f, 4 * g + j, kWave);
-#pragma unroll
-          for (int i = 0; i < D / 16; i++) B.o[i][j] *= fj;
-          B.z[j] *= fj;
-        }
-#pragma unroll
-        for (int t = 0; t < 2; t++)
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            d[t][j] = fmaf(xs[t][j], B.c1, fmaf(xz[t][j], B.c2, -ref));
-            if (tail) d[t][j] = key0 + 16 * t + 4 * g + j < B.limit ? d[t][j] : kNegInf;
-          }
-      }
-      float e[2][4];
+      for (int j = 0; j < 4; j++) top = fmaxf(top, d[b][t][j]);
+    if (__any(top > B.above)) {
+      top = fmaxf(top, shfl_xor(top, 16));
+      top = fmaxf(top, shfl_xor(top, 32));
+      const float up = top > B.above ? top - kHead : 0.f;
+      const float f = top > B.above && B.above != kUnset ? fast_exp2(-up) : 1.f;
+      B.above = top > B.above ? kSlack : B.above;
+      B.nref -= up;
 #pragma unroll
       for (int t = 0; t < 2; t++)
 #pragma unroll
-        for (int j = 0; j < 4; j++) e[t][j] = fast_exp2(d[t][j]);
-      p[b] = (u32x4){pack_f16(e[0][0], e[0][1]), pack_f16(e[0][2], e[0][3]), pack_f16(e[1][0], e[1][1]),
-                     pack_f16(e[1][2], e[1][3])};
-      B.z = mfma_f16(p[b], vz, B.z);
+        for (int j = 0; j < 4; j++) d[b][t][j] -= up;
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const float fj = __shfl(f, 4 * g + j, kWave);
+#pragma unroll
+        for (int i = 0; i < D / 16; i++) B.o[i][j] *= fj;
+        B.z[j] *= fj;
+      }
     }
+#pragma unroll
+    for (int t = 0; t < 2; t++) {
+      p[b][2 * t] = pack_f16(fast_exp2(d[b][t][0]), fast_exp2(d[b][t][1]));
+      p[b][2 * t + 1] = pack_f16(fast_exp2(d[b][t][2]), fast_exp2(d[b][t][3]));
+    }
+    B.z = mfma_f16(p[b], vz, B.z);
   }
-  // Values: half h of the codes has instances 4 h .. 4 h + 3, groups of 2 or 4 instances.
+  // Values: half h of the codes has instances 4 h .. 4 h + 3, in groups of 2 or 4 instances.
 #pragma unroll
   for (int h = 0; h < D / 64; h++) {
+    const u32x4 code = *reinterpret_cast<const u32x4 *>(slot + Q::VC + h * 1024 + lane * 16);
     u32x4 vb[4];
 #pragma unroll
     for (int r = 0; r < 4; r++) {
-      const u32x4 x = expand(c.v[h][r]);
+      const u32x4 x = expand(code[r]);
 #pragma unroll
       for (int i = 0; i < 4; i++) vb[i][r] = x[i];
     }
 #pragma unroll
     for (int b = 0; b < RB; b++) {
-      constexpr int IPG = QTile<D, NG>::GROUP / 16;  // instances per group
+      constexpr int IPG = Q::GROUP / 16;  // instances per group
       u32x4 ps;
 #pragma unroll
       for (int i = 0; i < 4; i++) {
         const int inst = 4 * h + i;
         if (inst % IPG == 0 || i == 0) {
 #pragma unroll
-          for (int r = 0; r < 4; r++) ps[r] = mul_f16(p[b][r], c.vs[inst / IPG][r]);
+          for (int r = 0; r < 4; r++) ps[r] = mul_f16(p[b][r], vs[inst / IPG][r]);
         }
         blk[b].o[inst] = mfma_f16(ps, vb[i], blk[b].o[inst]);
       }
@@ -560,10 +544,19 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], Chunk<D, NG> 
   }
 }
 
+// Waves per SIMD and tiles in a wave's ring. One wave's registers hold up to
+// three row blocks beside another's.
+template <int RB>
+constexpr int kCtxWaves = RB <= 3 ? 2 : 1;
+template <int RB>
+constexpr int kCtxDepth = RB <= 3 ? 3 : 6;
+
 // Context kernel: one wave per span.
 template <int D, int NG, int RB>
-__global__ __launch_bounds__(kWave) void quant_ctx(QuantAttnParams p) {
+__global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves<RB>))) void quant_ctx(QuantAttnParams p) {
   using Q = QTile<D, NG>;
+  constexpr int DEPTH = kCtxDepth<RB>, LOADS = Ring<D, NG>::LOADS, SLOT = Ring<D, NG>::SLOT;
+  __shared__ __align__(1024) char ring[DEPTH * SLOT];
   const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
   // The row groups of a span run eight workgroups apart, on one XCD.
   const int xcd = blockIdx.x & 7, k8 = blockIdx.x >> 3;
@@ -580,25 +573,22 @@ __global__ __launch_bounds__(kWave) void quant_ctx(QuantAttnParams p) {
     const int t = ctx_tiles(p, c0 + lane), sc = scan_tiles(t, lane);
     const uint64_t past = __ballot((at + sc) * lh > pos0);
     if (past) {
-      const int i = __ffsll((long long)past) - 1;
+      const int i = uniform(__ffsll((long long)past) - 1);
       c = c0 + i;
-      at += __shfl(sc - t, i, kWave);
+      at += uniform(__shfl(sc - t, i, kWave));
       break;
     }
-    at += __shfl(sc, kWave - 1, kWave);
+    at += uniform(__shfl(sc, kWave - 1, kWave));
   }
   long pos = pos0;
   int n_ctx = uniform(ctx_len(p, c)), tiles = (n_ctx + kQuantTile - 1) / kQuantTile;
-  int u = uniform((int)((pos - at * lh) / tiles));       // unit within the context
-  int tile = uniform((int)((pos - at * lh) % tiles));
-  const Offsets<D, NG> off(lane);
+  int u = (int)((pos - at * lh) / tiles);  // unit within the context
+  int tile = (int)((pos - at * lh) % tiles);
   Block<D, NG> blk[RB];
   while (pos < end) {
     const int last = (int)min((long)tiles, tile + (end - pos));
     const int l = u / p.Hkv, h = u % p.Hkv;
     const char *base = static_cast<const char *>(p.data) + ((size_t)c * lh + u) * p.ntiles * Q::BYTES;
-    Chunk<D, NG> a, b;
-    load_tile<D, NG>(a, base + (size_t)tile * Q::BYTES, true, off);
     int least = n_ctx;
 #pragma unroll
     for (int i = 0; i < RB; i++) {
@@ -617,12 +607,18 @@ __global__ __launch_bounds__(kWave) void quant_ctx(QuantAttnParams p) {
       for (int x = 8; x >= 1; x >>= 1) m = min(m, shfl_xor(m, x));
       least = min(least, uniform(m));
     }
-    for (int t = tile; t < last; t += 2) {
-      load_tile<D, NG>(b, base + (size_t)(t + 1) * Q::BYTES, t + 1 < last, off);
-      tile_step<D, NG, RB>(blk, a, t * Q::KEYS, n_ctx, (t + 1) * Q::KEYS > least, lane);
-      if (t + 1 >= last) break;
-      load_tile<D, NG>(a, base + (size_t)(t + 2) * Q::BYTES, t + 2 < last, off);
-      tile_step<D, NG, RB>(blk, b, (t + 1) * Q::KEYS, n_ctx, (t + 2) * Q::KEYS > least, lane);
+    // The queries' loads are done, so that the waits below count tiles alone.
+    wait_vm<0>();
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; i++)
+      load_tile<D, NG>(ring + i * SLOT, base + (size_t)(tile + i) * Q::BYTES, tile + i < last, lane);
+    int at_slot = 0;
+    for (int t = tile; t < last; t++) {
+      const int next = at_slot == 0 ? DEPTH - 1 : at_slot - 1, tn = t + DEPTH - 1;
+      load_tile<D, NG>(ring + next * SLOT, base + (size_t)tn * Q::BYTES, tn < last, lane);
+      wait_vm<LOADS *(DEPTH - 1)>();
+      tile_step<D, NG, RB>(blk, ring + at_slot * SLOT, t * Q::KEYS, n_ctx, (t + 1) * Q::KEYS > least, lane);
+      at_slot = at_slot + 1 == DEPTH ? 0 : at_slot + 1;
     }
     // The records of this piece.
     float *rec = p.ws + ((size_t)w + (size_t)c * lh + u) * rows * kRecFloats<D>;
@@ -632,7 +628,7 @@ __global__ __launch_bounds__(kWave) void quant_ctx(QuantAttnParams p) {
       for (int j = 0; j < 4; j++) {
         const int r = (rg * RB + i) * 16 + 4 * g + j;
         const float den = __shfl(blk[i].z[j], (lane & 48) + NG, kWave);
-        const float ref = __shfl(blk[i].ref, 4 * g + j, kWave);
+        const float ref = -__shfl(blk[i].nref, 4 * g + j, kWave);
         const float inv = den > 0.f ? 1.0f / den : 0.f;
         float off_j[NG];
 #pragma unroll
@@ -726,9 +722,9 @@ __global__ __launch_bounds__(kOwnWaves *kWave) void quant_join(QuantAttnParams p
     int t = c0 + lane < c ? ctx_tiles(p, c0 + lane) : 0;
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) t += shfl_xor(t, m);
-    before += t;
+    before += uniform(t);
   }
-  const int mine = ctx_tiles(p, c);
+  const int mine = uniform(ctx_tiles(p, c));
 
   if (u > 0) {
     const size_t own0 = (size_t)unit * p.ocap * D, new0 = (size_t)unit * p.nq * D;
@@ -923,7 +919,7 @@ __global__ __launch_bounds__(kOwnWaves *kWave) void quant_join(QuantAttnParams p
   }
 }
 
-constexpr int kChipWaves = 2048;  // two waves per SIMD: 256 CUs of four
+constexpr int kChipSimds = 1024;  // 256 CUs of four
 constexpr int kMinSpan = 4;
 constexpr int kMaxBlocks = 4;     // row blocks a wave takes at once
 
@@ -933,7 +929,8 @@ void plan(QuantAttnParams *p) {
   p->row_groups = (blocks + kMaxBlocks - 1) / kMaxBlocks;
   p->rb = (blocks + p->row_groups - 1) / p->row_groups;
   const double tiles = (double)p->P * p->L * p->Hkv * p->ntiles;
-  const int most = kChipWaves / p->row_groups > 64 ? kChipWaves / p->row_groups : 64;
+  const int waves = kChipSimds * (p->rb <= 3 ? kCtxWaves<3> : kCtxWaves<4>);
+  const int most = waves / p->row_groups > 64 ? waves / p->row_groups : 64;
   p->min_span = kMinSpan;
   const double want = tiles / kMinSpan + 1;
   p->nwaves = want < most ? (int)want : most;
