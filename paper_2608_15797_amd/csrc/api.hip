@@ -602,6 +602,8 @@ int quant_attn_shapes(const kvr_quant_cache *ctx, const kvr_cache *own, int32_t 
   p->C = p->S / p->P;
   p->ocap = own ? own->cap : 0;
   p->dtype = dtype; p->Hq = Hq; p->G = Hq / ctx->Hkv; p->nq = nq;
+  if ((double)p->P * p->L * p->Hkv * p->ntiles > 2147483647.0)
+    return fail(KVR_EUNSUPPORTED, "the contexts hold more than 2^31 tiles of 32 slots");
   if ((double)p->S * p->L * Hq * nq > 2147483647.0) return fail(KVR_EUNSUPPORTED, "S*L*Hq*nq exceeds the launch grid");
   return KVR_OK;
 }

@@ -221,8 +221,8 @@ struct QuantAttnParams {
   float *ws;
   // Plan of a bfloat16 call: row blocks per wave and groups of them, waves of
   // the context kernel and their least span in tiles, rows per workgroup of
-  // the join.
-  int rb, row_groups, nwaves, min_span, rpw;
+  // the join, or a wave each.
+  int rb, row_groups, nwaves, min_span, rpw, join_waves;
 };
 size_t quant_attn_workspace_bytes(const QuantAttnParams &p);
 hipError_t launch_quant_attn(const QuantAttnParams &p, hipStream_t stream);

@@ -250,11 +250,6 @@ __device__ __forceinline__ float4_t mfma_bf16(u32x4 a, u32x4 b, float4_t c) {
 }
 // Lane 0's value as a scalar.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ long uniform(long x) {
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32));
-  return (long)(((uint64_t)hi << 32) | lo);
-}
 
 // A partial record of one query row: (max, sum, -, -) in the log2 domain, then
 // o / sum as D float16.
@@ -268,18 +263,18 @@ constexpr int kRecFloats = 4 + D / 2;
 constexpr float kSlack = 4.0f, kHead = 3.0f;
 constexpr float kUnset = -3.0e38f;
 
-// How the tiles are cut: waves of `span` tiles over all units in order.
-struct Cut {
-  long span;
-  long total;
-};
-
 __device__ __forceinline__ int ctx_tiles(const QuantAttnParams &p, int c) {
   return c < p.P ? (ctx_len(p, c) + kQuantTile - 1) / kQuantTile : 0;
 }
 
-// Tiles of the contexts before c0 .. c0 + 63, inclusive scan over the lanes.
-__device__ __forceinline__ int scan_tiles(int t, int lane) {
+// How the tiles are cut: all units in order, `span` tiles to a wave. The host
+// has refused contexts of 2^31 tiles and more.
+struct Cut {
+  int span, total;  // in tiles
+  int first, sum;   // lane: tiles of context `lane`; of contexts 0 .. lane
+};
+
+__device__ __forceinline__ int scan_lanes(int t, int lane) {
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) {
     const int o = __shfl_up(t, off, kWave);
@@ -289,16 +284,14 @@ __device__ __forceinline__ int scan_tiles(int t, int lane) {
 }
 
 __device__ __forceinline__ Cut cut_of(const QuantAttnParams &p, int lane) {
-  long sum = 0;
-  for (int c0 = 0; c0 < p.P; c0 += kWave) {
-    int t = ctx_tiles(p, c0 + lane);
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) t += shfl_xor(t, m);
-    sum += t;
-  }
   Cut cut;
-  cut.total = uniform(sum) * p.L * p.Hkv;
-  cut.span = max((cut.total + p.nwaves - 1) / p.nwaves, (long)p.min_span);
+  cut.first = ctx_tiles(p, lane);
+  cut.sum = scan_lanes(cut.first, lane);
+  int sum = uniform(__shfl(cut.sum, kWave - 1, kWave));
+  for (int c0 = kWave; c0 < p.P; c0 += kWave)
+    sum += uniform(__shfl(scan_lanes(ctx_tiles(p, c0 + lane), lane), kWave - 1, kWave));
+  cut.total = sum * p.L * p.Hkv;
+  cut.span = max((int)(((uint32_t)cut.total + p.nwaves - 1) / (uint32_t)p.nwaves), p.min_span);
   return cut;
 }
 
@@ -311,13 +304,16 @@ __device__ __forceinline__ void wait_vm() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 
+// s_waitcnt lgkmcnt(0): this wave's reads of LDS have been answered.
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4)); }
+
 // A wave's ring of tiles in LDS. A tile is one block of memory, loaded as it
 // lies by LOADS instructions of 1 KiB (past the end of a unit: zeros, without
 // a memory access); the operands are read from there.
 template <int D, int NG>
 struct Ring {
   static constexpr int LOADS = (QTile<D, NG>::BYTES + 1023) / 1024;
-  static constexpr int SLOT = LOADS * 1024;
+  static constexpr int SLOT = QTile<D, NG>::BYTES;
 };
 
 template <int D, int NG>
@@ -325,8 +321,12 @@ __device__ __forceinline__ void load_tile(char *slot, const char *tile, bool liv
   const rsrc_t r = make_rsrc(tile, live ? QTile<D, NG>::BYTES : 0);
 #if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
-  for (int i = 0; i < Ring<D, NG>::LOADS; i++)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)(slot + i * 1024), 16, lane * 16, i * 1024, 0, kStreamLoad);
+  for (int i = 0; i < Ring<D, NG>::LOADS; i++) {
+    // The last instruction's lanes past the tile would write zeros behind it.
+    if ((i + 1) * 1024 <= QTile<D, NG>::BYTES || i * 1024 + lane * 16 < QTile<D, NG>::BYTES)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)(slot + i * 1024), 16, lane * 16, i * 1024, 0,
+                                               kStreamLoad);
+  }
 #else
   (void)r;  // the host pass has no buffer-to-LDS loads
 #endif
@@ -544,12 +544,21 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
   }
 }
 
+#ifndef JW
+#define JW 2
+#endif
+#ifndef DEP
+#define DEP 3
+#endif
+#ifndef OCC
+#define OCC 2
+#endif
 // Waves per SIMD and tiles in a wave's ring. One wave's registers hold up to
 // three row blocks beside another's.
 template <int RB>
-constexpr int kCtxWaves = RB <= 3 ? 2 : 1;
+constexpr int kCtxWaves = RB == 1 ? OCC : RB <= 3 ? 2 : 1;
 template <int RB>
-constexpr int kCtxDepth = RB <= 3 ? 3 : 6;
+constexpr int kCtxDepth = RB <= 3 ? DEP : 6;
 
 // Context kernel: one wave per span.
 template <int D, int NG, int RB>
@@ -563,32 +572,37 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves
   const int w = (k8 / p.row_groups) * 8 + xcd, rg = k8 % p.row_groups;
   if (w >= p.nwaves) return;
   const Cut cut = cut_of(p, lane);
-  const long pos0 = w * cut.span, end = min(pos0 + cut.span, cut.total);
-  if (pos0 >= end) return;
+  if ((long)w * cut.span >= cut.total) return;
+  int pos = w * cut.span;
+  const int end = min(pos + cut.span, cut.total);
   const int lh = p.L * p.Hkv, rows = p.C * p.nq * p.G, per = p.nq * p.G;
-  // The context that holds pos0.
-  int c = 0;
-  long at = 0;  // tiles before context c
-  for (int c0 = 0; c0 < p.P; c0 += kWave) {
-    const int t = ctx_tiles(p, c0 + lane), sc = scan_tiles(t, lane);
-    const uint64_t past = __ballot((at + sc) * lh > pos0);
+  // The context that holds the first tile, and the tiles before it.
+  int c = 0, at = 0, t = cut.first, sc = cut.sum;
+  for (;;) {
+    const uint64_t past = __ballot((at + sc) * lh > pos);
     if (past) {
       const int i = uniform(__ffsll((long long)past) - 1);
-      c = c0 + i;
+      c += i;
       at += uniform(__shfl(sc - t, i, kWave));
       break;
     }
     at += uniform(__shfl(sc, kWave - 1, kWave));
+    c += kWave;
+    t = ctx_tiles(p, c + lane);
+    sc = scan_lanes(t, lane);
   }
-  long pos = pos0;
   int n_ctx = uniform(ctx_len(p, c)), tiles = (n_ctx + kQuantTile - 1) / kQuantTile;
-  int u = (int)((pos - at * lh) / tiles);  // unit within the context
-  int tile = (int)((pos - at * lh) % tiles);
+  int u = (pos - at * lh) / tiles;  // unit within the context
+  int tile = (pos - at * lh) % tiles;
   Block<D, NG> blk[RB];
   while (pos < end) {
-    const int last = (int)min((long)tiles, tile + (end - pos));
+    const int last = min(tiles, tile + (end - pos));
     const int l = u / p.Hkv, h = u % p.Hkv;
     const char *base = static_cast<const char *>(p.data) + ((size_t)c * lh + u) * p.ntiles * Q::BYTES;
+    // The first tiles are on their way while the queries are made ready.
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; i++)
+      load_tile<D, NG>(ring + i * SLOT, base + (size_t)(tile + i) * Q::BYTES, tile + i < last, lane);
     int least = n_ctx;
 #pragma unroll
     for (int i = 0; i < RB; i++) {
@@ -598,7 +612,7 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves
       if (r < rows) {
         const int s = c * p.C + r / per, rr = r % per;
         row = static_cast<const bf16_t *>(p.q) + ((((size_t)s * p.L + l) * p.Hkv + h) * per + rr) * D;
-        blk[i].limit = (int)min((long)n_ctx, (long)n_ctx + own_len(p, s) - (p.nq - 1 - rr % p.nq));
+        if (p.nq > 1) blk[i].limit = (int)min((long)n_ctx, (long)n_ctx + own_len(p, s) - (p.nq - 1 - rr % p.nq));
       }
       load_queries<D, NG>(blk[i], p, row, lane);
       clear<D, NG>(blk[i]);
@@ -607,19 +621,20 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves
       for (int x = 8; x >= 1; x >>= 1) m = min(m, shfl_xor(m, x));
       least = min(least, uniform(m));
     }
-    // The queries' loads are done, so that the waits below count tiles alone.
+    // The queries' loads are done, so that the waits below count tiles alone
+    // (and with them the first tiles', which were issued before).
     wait_vm<0>();
-#pragma unroll
-    for (int i = 0; i < DEPTH - 1; i++)
-      load_tile<D, NG>(ring + i * SLOT, base + (size_t)(tile + i) * Q::BYTES, tile + i < last, lane);
     int at_slot = 0;
     for (int t = tile; t < last; t++) {
       const int next = at_slot == 0 ? DEPTH - 1 : at_slot - 1, tn = t + DEPTH - 1;
+      wait_lds();  // the slot's tile has been read
       load_tile<D, NG>(ring + next * SLOT, base + (size_t)tn * Q::BYTES, tn < last, lane);
       wait_vm<LOADS *(DEPTH - 1)>();
       tile_step<D, NG, RB>(blk, ring + at_slot * SLOT, t * Q::KEYS, n_ctx, (t + 1) * Q::KEYS > least, lane);
       at_slot = at_slot + 1 == DEPTH ? 0 : at_slot + 1;
     }
+    wait_vm<0>();  // the zeros behind the last tile, before the ring starts again
+    wait_lds();
     // The records of this piece.
     float *rec = p.ws + ((size_t)w + (size_t)c * lh + u) * rows * kRecFloats<D>;
 #pragma unroll
@@ -695,14 +710,258 @@ __device__ __forceinline__ void load_own(OwnChunk<D> &c, const OwnRows<bf16_t> &
   }
 }
 
+// A context's tiles and those before it.
+struct Place {
+  int tiles, before;
+};
+__device__ __forceinline__ Place place_of(const QuantAttnParams &p, const Cut &cut, int c, int lane) {
+  int t = cut.first, sc = cut.sum, before = 0, c0 = 0;
+  for (; c0 + kWave <= c; c0 += kWave) {
+    before += uniform(__shfl(sc, kWave - 1, kWave));
+    t = ctx_tiles(p, c0 + kWave + lane);
+    sc = scan_lanes(t, lane);
+  }
+  Place h;
+  h.tiles = uniform(__shfl(t, c - c0, kWave));
+  h.before = before + uniform(__shfl(sc - t, c - c0, kWave));
+  return h;
+}
+
+// What a wave has of the own rows: 16 query rows (lane's row: n), running
+// maximum and sum per row, o as rows 4 g + 0..3 at d = n D / 16 + b.
+template <int D>
+struct OwnState {
+  u32x4 q[D / 32];
+  int limit;  // keys that the lane's row sees
+  float m, den;
+  float4_t o[D / 16];
+};
+
+// The own rows of a unit and the query rows r0 .. r0 + nrow - 1 of its sequence.
+struct OwnUnit {
+  OwnRows<bf16_t> k, v;
+  int u, nq, r0, nrow;
+  float sl2;
+};
+
+template <int D>
+__device__ __forceinline__ OwnUnit own_unit(const QuantAttnParams &p, int unit, int u, int r0, int nrow) {
+  const size_t own0 = (size_t)unit * p.ocap * D, new0 = (size_t)unit * p.nq * D;
+  const bf16_t *fk = static_cast<const bf16_t *>(p.k_new), *fv = static_cast<const bf16_t *>(p.v_new);
+  return OwnUnit{{static_cast<const bf16_t *>(p.ok) + own0, fk ? fk + new0 : nullptr, u - p.nq},
+                 {static_cast<const bf16_t *>(p.ov) + own0, fv ? fv + new0 : nullptr, u - p.nq},
+                 u, p.nq, r0, nrow, p.scale * kLog2e};
+}
+
+template <int D>
+__device__ __forceinline__ void own_begin(OwnState<D> &st, const QuantAttnParams &p, const OwnUnit &w, int unit, int lane) {
+  const int n = lane & 15, g = lane >> 4, r = w.r0 + min(n, w.nrow - 1);
+  const bf16_t *row = static_cast<const bf16_t *>(p.q) + ((size_t)unit * p.nq * p.G + r) * D;
+#pragma unroll
+  for (int i = 0; i < D / 32; i++) st.q[i] = *reinterpret_cast<const u32x4 *>(row + 32 * i + 8 * g);
+  st.limit = w.u - (p.nq - 1 - r % p.nq);
+  st.m = kNegInf;
+  st.den = 0.f;
+#pragma unroll
+  for (int b = 0; b < D / 16; b++) st.o[b] = (float4_t){0.f, 0.f, 0.f, 0.f};
+}
+
+// The B operand of instance b from the values of the lane's 8 slots.
+template <int D>
+__device__ __forceinline__ u32x4 value_operand(const uint32_t (&v)[8][D / 32], int b) {
+  u32x4 w;
+#pragma unroll
+  for (int r = 0; r < 4; r++)
+    w[r] = __builtin_amdgcn_perm(v[2 * r + 1][b / 2], v[2 * r][b / 2], b & 1 ? 0x07060302u : 0x05040100u);
+  return w;
+}
+
+// One chunk. p is split into two bfloat16 terms, so that its rounding (2^-17)
+// stays out of the result.
+template <int D>
+__device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const OwnUnit &w, int key0, int lane) {
+  const int g = lane >> 4;
+  float x[2][4], top = kNegInf;
+#pragma unroll
+  for (int t = 0; t < 2; t++) {
+    float4_t a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < D / 32; i++) a = mfma_bf16(ch.k[t][i], st.q[i], a);
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      x[t][j] = key0 + 16 * t + 4 * g + j < st.limit ? a[j] * w.sl2 : kNegInf;
+      top = fmaxf(top, x[t][j]);
+    }
+  }
+  top = fmaxf(top, shfl_xor(top, 16));
+  top = fmaxf(top, shfl_xor(top, 32));
+  const float mn = fmaxf(st.m, top), ref = mn == kNegInf ? 0.f : mn;
+  if (__any(mn > st.m)) {
+    const float f = fast_exp2(st.m - ref);
+    st.den *= f;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      const float fj = __shfl(f, 4 * g + j, kWave);
+#pragma unroll
+      for (int b = 0; b < D / 16; b++) st.o[b][j] *= fj;
+    }
+  }
+  st.m = mn;
+  u32x4 hi, lo;
+#pragma unroll
+  for (int t = 0; t < 2; t++)
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+      const float e0 = fast_exp2(x[t][j] - ref), e1 = fast_exp2(x[t][j + 1] - ref);
+      st.den += e0 + e1;
+      const uint32_t h = pack_bf16x2(e0, e1);
+      hi[2 * t + j / 2] = h;
+      lo[2 * t + j / 2] = pack_bf16x2(e0 - bf16_lo(h), e1 - bf16_hi(h));
+    }
+  // Rows past the last live one hold anything; so may rows that only later
+  // queries see, where a value that is not finite would reach the others as 0
+  // times it: those get a product per query token.
+  const int sees_all = w.u - (w.nq - 1);
+  bool split = false;
+  if (key0 + 32 > sees_all) {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const int key = key0 + slot_key<D>(g, e);
+#pragma unroll
+      for (int i = 0; i < D / 32; i++) {
+        if (key >= w.u) ch.v[e][i] = 0u;
+        const uint32_t v = ch.v[e][i];
+        odd |= key >= sees_all && ((v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u);
+      }
+    }
+    split = __any(odd);
+  }
+  if (!split) {
+#pragma unroll
+    for (int b = 0; b < D / 16; b++) {
+      const u32x4 v = value_operand<D>(ch.v, b);
+      st.o[b] = mfma_bf16(lo, v, mfma_bf16(hi, v, st.o[b]));
+    }
+    return;
+  }
+#pragma unroll 1
+  for (int t = 0; t < w.nq; t++) {
+    const int lim = w.u - (w.nq - 1 - t);
+    uint32_t see[4];
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const int k0 = key0 + slot_key<D>(g, 2 * r);
+      see[r] = (k0 < lim ? 0xffffu : 0u) | (k0 + 1 < lim ? 0xffff0000u : 0u);
+    }
+#pragma unroll
+    for (int b = 0; b < D / 16; b++) {
+      u32x4 v = value_operand<D>(ch.v, b);
+#pragma unroll
+      for (int r = 0; r < 4; r++) v[r] &= see[r];
+      const float4_t acc = mfma_bf16(lo, v, mfma_bf16(hi, v, st.o[b]));
+#pragma unroll
+      for (int j = 0; j < 4; j++) st.o[b][j] = (w.r0 + 4 * g + j) % w.nq == t ? acc[j] : st.o[b][j];
+    }
+  }
+}
+
+// Joins (mr, lr, values x whose sum of weights is lr after the factor scale) to a row's (m, den, o).
+template <int EL>
+__device__ __forceinline__ void fold(float &m, float &den, float (&o)[EL], float mr, float lr, float scale,
+                                     const float (&x)[EL]) {
+  const float mn = fmaxf(m, mr);
+  const float fa = m == kNegInf ? 0.f : fast_exp2(m - mn), fb = lr == 0.f ? 0.f : fast_exp2(mr - mn);
+  m = mn;
+  den = den * fa + lr * fb;
+  const float sb = scale * fb;
+#pragma unroll
+  for (int e = 0; e < EL; e++) o[e] = fmaf(x[e], sb, o[e] * fa);
+}
+
+// Elements sub EL .. of a record's values.
+template <int EL>
+__device__ __forceinline__ void record_values(const float *rec, int sub, float (&x)[EL]) {
+  const f16_t *h = reinterpret_cast<const f16_t *>(rec + 4) + sub * EL;
+#pragma unroll
+  for (int e = 0; e < EL; e++) x[e] = (float)h[e];
+}
+
+template <int EL>
+__device__ __forceinline__ void put_row(bf16_t *row, int sub, const float (&o)[EL], float den) {
+  const float inv = den == 0.f ? 0.f : 1.0f / den;
+  uint32_t *to = reinterpret_cast<uint32_t *>(row) + sub * (EL / 2);
+#pragma unroll
+  for (int e = 0; e < EL; e += 2) to[e / 2] = pack_bf16x2(o[e] * inv, o[e + 1] * inv);
+}
+
+// Second kernel, many units: a wave per (sequence, layer, KV head) and 16 of
+// its rows attends to the own rows, 32 keys at a time, and joins the context's
+// records as it holds its result: 16 lanes per row, four rows per lane.
+template <int D, int NG>
+__global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(JW))) void quant_join_wave(QuantAttnParams p) {
+  constexpr int EL = D / 16;
+  const int per = p.nq * p.G, blocks = (per + 15) / 16;
+  const int unit = blockIdx.x / blocks, r0 = blockIdx.x % blocks * 16;
+  const int lh = p.L * p.Hkv, s = unit / lh, c = s / p.C;
+  const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
+  const int u = uniform(own_len(p, s)), nrow = min(16, per - r0);
+  OwnState<D> st;
+  st.m = kNegInf;
+  st.den = 0.f;
+#pragma unroll
+  for (int b = 0; b < D / 16; b++) st.o[b] = (float4_t){0.f, 0.f, 0.f, 0.f};
+  const OwnUnit w = own_unit<D>(p, unit, u, r0, nrow);
+  OwnChunk<D> ch;
+  if (u > 0) {
+    load_own<D>(ch, w.k, w.v, 0, u, lane);
+    own_begin<D>(st, p, w, unit, lane);
+  }
+  const Cut cut = cut_of(p, lane);
+  const Place here = place_of(p, cut, c, lane);
+  for (int key0 = 0; key0 < u; key0 += 32) {
+    if (key0) load_own<D>(ch, w.k, w.v, key0, u, lane);
+    own_step<D>(st, ch, w, key0, lane);
+  }
+  if (p.ok && r0 == 0) store_new<bf16_t, D, kWave>(p, unit, s, u);
+  st.den += shfl_xor(st.den, 16);
+  st.den += shfl_xor(st.den, 32);
+  const int first = here.before * lh + unit % lh * here.tiles;
+  const int w0 = first / cut.span, w1 = here.tiles > 0 ? (first + here.tiles - 1) / cut.span : w0 - 1;
+  const int rows = p.C * per;
+  const float *rec = p.ws + (((size_t)w0 + (size_t)c * lh + unit % lh) * rows + (s % p.C * per + r0)) * kRecFloats<D>;
+  float m[4], den[4], o[4][EL];
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    m[j] = __shfl(st.m, 4 * g + j, kWave);
+    den[j] = __shfl(st.den, 4 * g + j, kWave);
+#pragma unroll
+    for (int e = 0; e < EL; e++) o[j][e] = st.o[e][j];
+  }
+  for (int k = w0; k <= w1; k++, rec += (size_t)rows * kRecFloats<D>) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      const float *r = rec + (size_t)min(4 * g + j, nrow - 1) * kRecFloats<D>;
+      const float2_t ml = *reinterpret_cast<const float2_t *>(r);
+      float x[EL];
+      record_values<EL>(r, n, x);
+      fold<EL>(m[j], den[j], o[j], ml[0], ml[1], ml[1], x);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; j++)
+    if (4 * g + j < nrow)
+      put_row<EL>(static_cast<bf16_t *>(p.out) + ((size_t)unit * per + r0 + 4 * g + j) * D, n, o[j], den[j]);
+}
+
 constexpr int kOwnWaves = 4;
 
-// Second kernel: one workgroup per (sequence, layer, KV head) and rpw of its
-// rows. Its waves attend to the own rows (32 keys at a time, in turn), with p
-// as two bfloat16 terms; then all of them join these and the context's
-// records: 16 lanes per row, the records of a row dealt to 16 / rpw groups.
+// Second kernel, few units: a workgroup per (sequence, layer, KV head) and rpw
+// of its rows. Its waves attend to the own rows, 32 keys each in turn; then
+// all of them join these and the context's records: 16 lanes per row, the
+// records of a row dealt to 16 / rpw groups.
 template <int D, int NG>
-__global__ __launch_bounds__(kOwnWaves *kWave) void quant_join(QuantAttnParams p) {
+__global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_eu(2))) void quant_join(QuantAttnParams p) {
   constexpr int NT = kOwnWaves * kWave, EL = D / 16;  // elements per thread of the join
   __shared__ float so[kOwnWaves][16][D];
   __shared__ float sm[16][2];
@@ -716,154 +975,38 @@ __global__ __launch_bounds__(kOwnWaves *kWave) void quant_join(QuantAttnParams p
   if (p.ok && r0 == 0) store_new<bf16_t, D, NT>(p, unit, s, u);
 
   const Cut cut = cut_of(p, lane);
-  // Tiles before this context.
-  long before = 0;
-  for (int c0 = 0; c0 < c; c0 += kWave) {
-    int t = c0 + lane < c ? ctx_tiles(p, c0 + lane) : 0;
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) t += shfl_xor(t, m);
-    before += uniform(t);
-  }
-  const int mine = uniform(ctx_tiles(p, c));
+  const Place here = place_of(p, cut, c, lane);
 
   if (u > 0) {
-    const size_t own0 = (size_t)unit * p.ocap * D, new0 = (size_t)unit * p.nq * D;
-    const bf16_t *fk = static_cast<const bf16_t *>(p.k_new), *fv = static_cast<const bf16_t *>(p.v_new);
-    const OwnRows<bf16_t> K{static_cast<const bf16_t *>(p.ok) + own0, fk ? fk + new0 : nullptr, u - p.nq};
-    const OwnRows<bf16_t> V{static_cast<const bf16_t *>(p.ov) + own0, fv ? fv + new0 : nullptr, u - p.nq};
-    u32x4 q[D / 32];
-    const bf16_t *row = static_cast<const bf16_t *>(p.q) + ((size_t)unit * per + r0 + min(n, nrow - 1)) * D;
-#pragma unroll
-    for (int i = 0; i < D / 32; i++) q[i] = *reinterpret_cast<const u32x4 *>(row + 32 * i + 8 * g);
-    const int limit = u - (p.nq - 1 - (r0 + min(n, nrow - 1)) % p.nq);  // of the lane's row
-    const float sl2 = p.scale * kLog2e;
-    float m = kNegInf, den = 0.f;
-    float4_t o[D / 16];
-#pragma unroll
-    for (int b = 0; b < D / 16; b++) o[b] = (float4_t){0.f, 0.f, 0.f, 0.f};
+    const OwnUnit w = own_unit<D>(p, unit, u, r0, nrow);
+    OwnState<D> st;
+    own_begin<D>(st, p, w, unit, lane);
     for (int key0 = wave * 32; key0 < u; key0 += kOwnWaves * 32) {
       OwnChunk<D> ch;
-      load_own<D>(ch, K, V, key0, u, lane);
-      float x[2][4], top = kNegInf;
-#pragma unroll
-      for (int t = 0; t < 2; t++) {
-        float4_t a = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < D / 32; i++) a = mfma_bf16(ch.k[t][i], q[i], a);
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          x[t][j] = key0 + 16 * t + 4 * g + j < limit ? a[j] * sl2 : kNegInf;
-          top = fmaxf(top, x[t][j]);
-        }
-      }
-      top = fmaxf(top, shfl_xor(top, 16));
-      top = fmaxf(top, shfl_xor(top, 32));
-      const float mn = fmaxf(m, top), ref = mn == kNegInf ? 0.f : mn;
-      const float f = fast_exp2(m - ref);
-      m = mn;
-      den *= f;
-#pragma unroll
-      for (int j = 0; j < 4; j++) {
-        const float fj = __shfl(f, 4 * g + j, kWave);
-#pragma unroll
-        for (int b = 0; b < D / 16; b++) o[b][j] *= fj;
-      }
-      u32x4 hi, lo;
-#pragma unroll
-      for (int t = 0; t < 2; t++)
-#pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-          const float e0 = fast_exp2(x[t][j] - ref), e1 = fast_exp2(x[t][j + 1] - ref);
-          den += e0 + e1;
-          const uint32_t w = pack_bf16x2(e0, e1);
-          hi[2 * t + j / 2] = w;
-          lo[2 * t + j / 2] = pack_bf16x2(e0 - bf16_lo(w), e1 - bf16_hi(w));
-        }
-      // Rows past the last live one hold anything; so may rows that only later
-      // queries see, where a value that is not finite would reach the others
-      // as 0 times it: those get a product per query token.
-      const int sees_all = u - (p.nq - 1);
-      bool split = false;
-      if (key0 + 32 > sees_all) {
-        bool odd = false;
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          const int key = key0 + slot_key<D>(g, e);
-#pragma unroll
-          for (int i = 0; i < D / 32; i++) {
-            if (key >= u) ch.v[e][i] = 0u;
-            const uint32_t w = ch.v[e][i];
-            odd |= key >= sees_all && ((w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u);
-          }
-        }
-        split = __any(odd);
-      }
-      auto product = [&](const uint32_t (&v)[8][D / 32], float4_t (&acc)[D / 16]) {
-#pragma unroll
-        for (int b = 0; b < D / 16; b++) {
-          u32x4 w;
-#pragma unroll
-          for (int r = 0; r < 4; r++)
-            w[r] = __builtin_amdgcn_perm(v[2 * r + 1][b / 2], v[2 * r][b / 2], b & 1 ? 0x07060302u : 0x05040100u);
-          acc[b] = mfma_bf16(hi, w, acc[b]);
-          acc[b] = mfma_bf16(lo, w, acc[b]);
-        }
-      };
-      if (!split) {
-        product(ch.v, o);
-      } else {
-        for (int t = 0; t < p.nq; t++) {
-          const int lim = u - (p.nq - 1 - t);
-          uint32_t v[8][D / 32];
-          float4_t acc[D / 16];
-#pragma unroll
-          for (int e = 0; e < 8; e++)
-#pragma unroll
-            for (int i = 0; i < D / 32; i++) v[e][i] = key0 + slot_key<D>(g, e) < lim ? ch.v[e][i] : 0u;
-#pragma unroll
-          for (int b = 0; b < D / 16; b++) acc[b] = o[b];
-          product(v, acc);
-#pragma unroll
-          for (int j = 0; j < 4; j++)
-            if ((r0 + 4 * g + j) % p.nq == t) {
-#pragma unroll
-              for (int b = 0; b < D / 16; b++) o[b][j] = acc[b][j];
-            }
-        }
-      }
+      load_own<D>(ch, w.k, w.v, key0, u, lane);
+      own_step<D>(st, ch, w, key0, lane);
     }
-    den += shfl_xor(den, 16);
-    den += shfl_xor(den, 32);
+    st.den += shfl_xor(st.den, 16);
+    st.den += shfl_xor(st.den, 32);
     if (g == 0) {
-      wm[wave][n] = m;
-      wl[wave][n] = den;
+      wm[wave][n] = st.m;
+      wl[wave][n] = st.den;
     }
 #pragma unroll
     for (int j = 0; j < 4; j++)
 #pragma unroll
       for (int b = 0; b < D / 16; b += 4)
         *reinterpret_cast<float4_t *>(&so[wave][4 * g + j][n * EL + b]) =
-            (float4_t){o[b][j], o[b + 1][j], o[b + 2][j], o[b + 3][j]};
+            (float4_t){st.o[b][j], st.o[b + 1][j], st.o[b + 2][j], st.o[b + 3][j]};
   }
   __syncthreads();
 
-  // Join. Thread: row r0 + slot % rpw, records part, part + parts, .. of it, elements sub * EL ..
+  // Join. Thread: row r0 + slot % rpw, records part, part + parts, .. of it, elements sub EL ..
   const int slot = tid / 16, sub = tid % 16, parts = 16 / p.rpw;
   const int row = slot % p.rpw, part = slot / p.rpw;
   float m = kNegInf, den = 0.f, o[EL];
 #pragma unroll
   for (int e = 0; e < EL; e++) o[e] = 0.f;
-  auto fold = [&](float mr, float lr, float scale, const float (&x)[EL]) {
-    // lr: weight of the record's sum; scale: of its (unnormalised) values.
-    if (lr == 0.f) return;
-    const float mn = fmaxf(m, mr);
-    const float fa = m == kNegInf ? 0.f : fast_exp2(m - mn), fb = fast_exp2(mr - mn);
-    m = mn;
-    den = den * fa + lr * fb;
-    const float sb = scale * fb;
-#pragma unroll
-    for (int e = 0; e < EL; e++) o[e] = fmaf(x[e], sb, o[e] * fa);
-  };
   if (row < nrow) {
     if (part == 0 && u > 0) {
 #pragma unroll
@@ -871,22 +1014,20 @@ __global__ __launch_bounds__(kOwnWaves *kWave) void quant_join(QuantAttnParams p
         float x[EL];
 #pragma unroll
         for (int e = 0; e < EL; e++) x[e] = so[w][row][sub * EL + e];
-        fold(wm[w][row], wl[w][row], 1.f, x);
+        fold<EL>(m, den, o, wm[w][row], wl[w][row], 1.f, x);
       }
     }
-    if (mine > 0) {
-      const long first = (before * lh + (long)(unit % lh) * mine), w0 = first / cut.span,
-                 w1 = (first + mine - 1) / cut.span;
+    if (here.tiles > 0) {
+      const int first = here.before * lh + unit % lh * here.tiles;
+      const int w0 = first / cut.span, w1 = (first + here.tiles - 1) / cut.span;
       const int rows = p.C * per, r = s % p.C * per + r0 + row;
-      const size_t cu = (size_t)c * lh + unit % lh;
-      for (long w = w0 + part; w <= w1; w += parts) {
-        const float *rec = p.ws + ((size_t)w + cu) * rows * kRecFloats<D> + (size_t)r * kRecFloats<D>;
+      const float *rec = p.ws + (((size_t)(w0 + part) + (size_t)c * lh + unit % lh) * rows + r) * kRecFloats<D>;
+#pragma unroll 4
+      for (int k = w0 + part; k <= w1; k += parts, rec += (size_t)parts * rows * kRecFloats<D>) {
         const float2_t ml = *reinterpret_cast<const float2_t *>(rec);
         float x[EL];
-        const f16_t *h = reinterpret_cast<const f16_t *>(rec + 4) + sub * EL;
-#pragma unroll
-        for (int e = 0; e < EL; e++) x[e] = (float)h[e];
-        fold(ml[0], ml[1], ml[1], x);
+        record_values<EL>(rec, sub, x);
+        fold<EL>(m, den, o, ml[0], ml[1], ml[1], x);
       }
     }
   }
@@ -906,17 +1047,12 @@ __global__ __launch_bounds__(kOwnWaves *kWave) void quant_join(QuantAttnParams p
         const int from = k * p.rpw + row;
 #pragma unroll
         for (int e = 0; e < EL; e++) x[e] = po[from * D + sub * EL + e];
-        fold(sm[from][0], sm[from][1], 1.f, x);
+        fold<EL>(m, den, o, sm[from][0], sm[from][1], 1.f, x);
       }
     }
   }
-  if (part == 0 && row < nrow) {
-    const float inv = den == 0.f ? 0.f : 1.0f / den;
-    uint32_t *to = reinterpret_cast<uint32_t *>(static_cast<bf16_t *>(p.out) + ((size_t)unit * per + r0 + row) * D) +
-                   sub * (EL / 2);
-#pragma unroll
-    for (int e = 0; e < EL; e += 2) to[e / 2] = pack_bf16x2(o[e] * inv, o[e + 1] * inv);
-  }
+  if (part == 0 && row < nrow)
+    put_row<EL>(static_cast<bf16_t *>(p.out) + ((size_t)unit * per + r0 + row) * D, sub, o, den);
 }
 
 constexpr int kChipSimds = 1024;  // 256 CUs of four
@@ -929,15 +1065,18 @@ void plan(QuantAttnParams *p) {
   p->row_groups = (blocks + kMaxBlocks - 1) / kMaxBlocks;
   p->rb = (blocks + p->row_groups - 1) / p->row_groups;
   const double tiles = (double)p->P * p->L * p->Hkv * p->ntiles;
-  const int waves = kChipSimds * (p->rb <= 3 ? kCtxWaves<3> : kCtxWaves<4>);
+  const int waves = kChipSimds * (p->rb == 1 ? kCtxWaves<1> : p->rb <= 3 ? kCtxWaves<3> : kCtxWaves<4>);
   const int most = waves / p->row_groups > 64 ? waves / p->row_groups : 64;
   p->min_span = kMinSpan;
   const double want = tiles / kMinSpan + 1;
   p->nwaves = want < most ? (int)want : most;
-  // Fewer rows per workgroup of the join where there are few of them.
+  // The join: a wave each where that fills the chip; else workgroups, of
+  // fewer rows where there are few of them.
   const int per = p->nq * p->G;
+  const long units = (long)p->S * p->L * p->Hkv;
+  p->join_waves = units * ((per + 15) / 16) >= kChipSimds;
   int rpw = 16;
-  while (rpw > 1 && (long)p->S * p->L * p->Hkv * ((per + rpw - 1) / rpw) < 512) rpw /= 2;
+  while (rpw > 1 && units * ((per + rpw - 1) / rpw) < 512) rpw /= 2;
   p->rpw = rpw;
 }
 
@@ -955,9 +1094,10 @@ void launch_bf16(const QuantAttnParams &p, hipStream_t stream) {
     case 3: launch_ctx<D, NG, 3>(p, stream); break;
     default: launch_ctx<D, NG, 4>(p, stream); break;
   }
-  const int per = p.nq * p.G;
-  const uint32_t groups = (uint32_t)p.S * p.L * p.Hkv * ((per + p.rpw - 1) / p.rpw);
-  hipLaunchKernelGGL((quant_join<D, NG>), dim3(groups), dim3(kOwnWaves * kWave), 0, stream, p);
+  const int per = p.nq * p.G, rpw = p.join_waves ? 16 : p.rpw;
+  const dim3 groups((uint32_t)p.S * p.L * p.Hkv * ((per + rpw - 1) / rpw));
+  if (p.join_waves) hipLaunchKernelGGL((quant_join_wave<D, NG>), groups, dim3(kWave), 0, stream, p);
+  else hipLaunchKernelGGL((quant_join<D, NG>), groups, dim3(kOwnWaves * kWave), 0, stream, p);
 }
 
 template <int D, int NG>
