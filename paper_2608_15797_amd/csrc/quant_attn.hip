@@ -259,13 +259,17 @@ constexpr int kRecFloats = 4 + D / 2;
 // The running reference of a row's exponents is moved where a logit exceeds it
 // by more than kSlack (log2), to kHead below the largest: p stays at most 16,
 // so that p s fits float16 (s <= 2184.6), and is rarely far below 1, where
-// float16 gets coarse. kUnset: no reference yet, any logit sets it.
+// float16 gets coarse. The first tile of a piece sets it: a row that sees no
+// key there sees none later.
 constexpr float kSlack = 4.0f, kHead = 3.0f;
-constexpr float kUnset = -3.0e38f;
 
 __device__ __forceinline__ int ctx_tiles(const QuantAttnParams &p, int c) {
   return c < p.P ? (ctx_len(p, c) + kQuantTile - 1) / kQuantTile : 0;
 }
+
+// The workspace: the cut (1 + P ints, to a multiple of 16 bytes), the records.
+__host__ __device__ __forceinline__ size_t cut_floats(int P) { return ((size_t)P + 4) / 4 * 4; }
+__device__ __forceinline__ float *records(const QuantAttnParams &p) { return p.ws + cut_floats(p.P); }
 
 // How the tiles are cut: all units in order, `span` tiles to a wave. The host
 // has refused contexts of 2^31 tiles and more.
@@ -295,6 +299,22 @@ __device__ __forceinline__ Cut cut_of(const QuantAttnParams &p, int lane) {
   return cut;
 }
 
+// The cut for the second kernel, before the records: the span, then the tiles
+// before each context.
+__device__ __forceinline__ void store_cut(const QuantAttnParams &p, const Cut &cut, int lane) {
+  int *to = reinterpret_cast<int *>(p.ws);
+  if (lane == 0) to[0] = cut.span;
+  int t = cut.first, sc = cut.sum, at = 0;
+  for (int c0 = 0;;) {
+    if (c0 + lane < p.P) to[1 + c0 + lane] = at + sc - t;
+    at += uniform(__shfl(sc, kWave - 1, kWave));
+    c0 += kWave;
+    if (c0 >= p.P) break;
+    t = ctx_tiles(p, c0 + lane);
+    sc = scan_lanes(t, lane);
+  }
+}
+
 typedef __attribute__((address_space(3))) void lds_void_t;
 
 // s_waitcnt vmcnt(N), other counters unconstrained.
@@ -318,18 +338,16 @@ struct Ring {
 
 template <int D, int NG>
 __device__ __forceinline__ void load_tile(char *slot, const char *tile, bool live, int lane) {
-  const rsrc_t r = make_rsrc(tile, live ? QTile<D, NG>::BYTES : 0);
 #if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
   for (int i = 0; i < Ring<D, NG>::LOADS; i++) {
     // The last instruction's lanes past the tile would write zeros behind it.
-    if ((i + 1) * 1024 <= QTile<D, NG>::BYTES || i * 1024 + lane * 16 < QTile<D, NG>::BYTES)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)(slot + i * 1024), 16, lane * 16, i * 1024, 0,
-                                               kStreamLoad);
+    constexpr int BYTES = QTile<D, NG>::BYTES;
+    const rsrc_t r = make_rsrc(tile + i * 1024, live ? BYTES - i * 1024 : 0);
+    if ((i + 1) * 1024 <= BYTES || i * 1024 + lane * 16 < BYTES)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)(slot + i * 1024), 16, lane * 16, 0, 0, kStreamLoad);
   }
-#else
-  (void)r;  // the host pass has no buffer-to-LDS loads
-#endif
+#endif  // the host pass has no buffer-to-LDS loads
 }
 
 // The query operands of one row block and what is summed for it.
@@ -337,10 +355,9 @@ template <int D, int NG>
 struct Block {
   u32x4 q[D / 32];      // B operand of step i
   u32x2 qz;             // B operand of the offsets' product
-  float c1, c2;         // logits (log2) = c1 codes' part + c2 offsets' part
-  int limit;            // visible keys of the lane's row
+  float unit;           // logits (log2) = unit (2^24 codes' part + offsets' part)
   float nref;           // minus the exponents' reference of the lane's row
-  float above;          // a logit this much above the reference moves it
+  int limit;            // visible keys of the lane's row
   float4_t o[D / 16];   // rows 4 g + 0..3, column n of instance b
   float4_t z;           // the same rows; column: group's offsets, NG: sum of p
 };
@@ -397,24 +414,32 @@ __device__ __forceinline__ void load_queries(Block<D, NG> &b, const QuantAttnPar
   const float hi = (float)(f16_t)mine, mid = (float)(f16_t)(mine - hi);
   b.qz[0] = pack_f16(hi, mid);
   b.qz[1] = pack_f16(mine - hi - mid, 0.f);
-  b.c2 = ldexpf(p.scale * kLog2e, e);
-  b.c1 = ldexpf(p.scale * kLog2e, e + 24);
+  b.unit = ldexpf(p.scale * kLog2e, e);
 }
 
 template <int D, int NG>
 __device__ __forceinline__ void clear(Block<D, NG> &b) {
   b.nref = 0.f;
-  b.above = kUnset;
 #pragma unroll
   for (int i = 0; i < D / 16; i++) b.o[i] = (float4_t){0.f, 0.f, 0.f, 0.f};
   b.z = (float4_t){0.f, 0.f, 0.f, 0.f};
 }
 
+// Halfword mask of the lane's slots 2 r and 2 r + 1: all ones where the key is live.
+__device__ __forceinline__ uint32_t live_slots(int key0, int r, int g, int n_ctx) {
+  const int k0 = key0 + (r < 2 ? 4 * g + 2 * r : 16 + 4 * g + 2 * (r - 2));
+  return (k0 < n_ctx ? 0xffffu : 0u) | (k0 + 1 < n_ctx ? 0xffff0000u : 0u);
+}
+
+// Between the phases of a tile: what a phase loads from LDS is not held in
+// registers through the one before it.
+__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
+
 // One tile for RB row blocks; key0: the tile's first key; tail: some row does
 // not see some of its keys, or it has slots past the context's last.
 template <int D, int NG, int RB>
 __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *slot, int key0, int n_ctx, bool tail,
-                                          int lane) {
+                                          bool first, const int *limits, int lane) {
   using Q = QTile<D, NG>;
   const int n = lane & 15, g = lane >> 4;
   float d[RB][2][4];  // logits less the rows' references (log2)
@@ -451,14 +476,12 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
       }
 #pragma unroll
       for (int j = 0; j < 4; j++) {
-        d[b][t][j] = fmaf(xs[j], B.c1, fmaf(zt[j], B.c2, B.nref));
+        d[b][t][j] = fmaf(fmaf(xs[j], 0x1p24f, zt[j]), B.unit, B.nref);
       }
     }
   }
-  u32x4 vs[NG], vz;
-#pragma unroll
-  for (int i = 0; i < NG; i++) vs[i] = *reinterpret_cast<const u32x4 *>(slot + Q::VS + i * 64 + g * 16);
-  vz = *reinterpret_cast<const u32x4 *>(slot + Q::VZ + (n & (NG - 1)) * 64 + g * 16);
+  phase();
+  u32x4 vz = *reinterpret_cast<const u32x4 *>(slot + Q::VZ + (n & (NG - 1)) * 64 + g * 16);
   if (tail) {
     asm volatile("");  // a branch, not selects in every tile
 #pragma unroll
@@ -467,16 +490,10 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
       for (int t = 0; t < 2; t++)
 #pragma unroll
         for (int j = 0; j < 4; j++)
-          d[b][t][j] = key0 + 16 * t + 4 * g + j < blk[b].limit ? d[b][t][j] : kNegInf;
+          d[b][t][j] = key0 + 16 * t + 4 * g + j < (RB <= 2 ? blk[b].limit : limits[16 * b + n]) ? d[b][t][j] : kNegInf;
     // Slots past the last hold anything: their scales and offsets become 0.
 #pragma unroll
-    for (int r = 0; r < 4; r++) {
-      const int k0 = key0 + (r < 2 ? 4 * g + 2 * r : 16 + 4 * g + 2 * (r - 2));
-      const uint32_t m = (k0 < n_ctx ? 0xffffu : 0u) | (k0 + 1 < n_ctx ? 0xffff0000u : 0u);
-#pragma unroll
-      for (int i = 0; i < NG; i++) vs[i][r] &= m;
-      vz[r] &= m;
-    }
+    for (int r = 0; r < 4; r++) vz[r] &= live_slots(key0, r, g, n_ctx);
   }
   // Column NG holds ones; what the columns after it hold is not used.
 #pragma unroll
@@ -490,12 +507,12 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
     for (int t = 0; t < 2; t++)
 #pragma unroll
       for (int j = 0; j < 4; j++) top = fmaxf(top, d[b][t][j]);
-    if (__any(top > B.above)) {
+    if (first || __any(top > kSlack)) {
       top = fmaxf(top, shfl_xor(top, 16));
       top = fmaxf(top, shfl_xor(top, 32));
-      const float up = top > B.above ? top - kHead : 0.f;
-      const float f = top > B.above && B.above != kUnset ? fast_exp2(-up) : 1.f;
-      B.above = top > B.above ? kSlack : B.above;
+      const bool move = first ? top > kNegInf : top > kSlack;
+      const float up = move ? top - kHead : 0.f;
+      const float f = first ? 1.f : fast_exp2(-up);
       B.nref -= up;
 #pragma unroll
       for (int t = 0; t < 2; t++)
@@ -516,9 +533,23 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
     }
     B.z = mfma_f16(p[b], vz, B.z);
   }
-  // Values: half h of the codes has instances 4 h .. 4 h + 3, in groups of 2 or 4 instances.
+  phase();
+  // Values: half h of the codes has instances 4 h .. 4 h + 3, in GH groups.
 #pragma unroll
   for (int h = 0; h < D / 64; h++) {
+    constexpr int IPG = Q::GROUP / 16, GH = 4 / IPG;  // instances per group
+    u32x4 vs[GH];
+#pragma unroll
+    for (int i = 0; i < GH; i++) vs[i] = *reinterpret_cast<const u32x4 *>(slot + Q::VS + (h * GH + i) * 64 + g * 16);
+    if (tail) {
+      asm volatile("");
+#pragma unroll
+      for (int r = 0; r < 4; r++) {
+        const uint32_t m = live_slots(key0, r, g, n_ctx);
+#pragma unroll
+        for (int i = 0; i < GH; i++) vs[i][r] &= m;
+      }
+    }
     const u32x4 code = *reinterpret_cast<const u32x4 *>(slot + Q::VC + h * 1024 + lane * 16);
     u32x4 vb[4];
 #pragma unroll
@@ -529,14 +560,13 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
     }
 #pragma unroll
     for (int b = 0; b < RB; b++) {
-      constexpr int IPG = Q::GROUP / 16;  // instances per group
       u32x4 ps;
 #pragma unroll
       for (int i = 0; i < 4; i++) {
         const int inst = 4 * h + i;
-        if (inst % IPG == 0 || i == 0) {
+        if (i % IPG == 0) {
 #pragma unroll
-          for (int r = 0; r < 4; r++) ps[r] = mul_f16(p[b][r], vs[inst / IPG][r]);
+          for (int r = 0; r < 4; r++) ps[r] = mul_f16(p[b][r], vs[i / IPG][r]);
         }
         blk[b].o[inst] = mfma_f16(ps, vb[i], blk[b].o[inst]);
       }
@@ -544,21 +574,14 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
   }
 }
 
-#ifndef JW
-#define JW 2
-#endif
-#ifndef DEP
-#define DEP 3
-#endif
-#ifndef OCC
-#define OCC 2
-#endif
 // Waves per SIMD and tiles in a wave's ring. One wave's registers hold up to
-// three row blocks beside another's.
+// three row blocks beside another's; two waves' rings of four 5 KiB tiles each
+// are all of a CU's LDS. 32 contexts of 16384 in groups of 64: rings of two,
+// three and four tiles 620, 656 and 588 us, three waves with two tiles 590.
 template <int RB>
-constexpr int kCtxWaves = RB == 1 ? OCC : RB <= 3 ? 2 : 1;
+constexpr int kCtxWaves = RB <= 3 ? 2 : 1;
 template <int RB>
-constexpr int kCtxDepth = RB <= 3 ? DEP : 6;
+constexpr int kCtxDepth = RB <= 2 ? 4 : RB == 3 ? 3 : 6;
 
 // Context kernel: one wave per span.
 template <int D, int NG, int RB>
@@ -566,12 +589,14 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves
   using Q = QTile<D, NG>;
   constexpr int DEPTH = kCtxDepth<RB>, LOADS = Ring<D, NG>::LOADS, SLOT = Ring<D, NG>::SLOT;
   __shared__ __align__(1024) char ring[DEPTH * SLOT];
+  __shared__ int limits[RB <= 2 ? 1 : RB * 16];  // visible keys of each row, beyond two blocks (registers)
   const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
   // The row groups of a span run eight workgroups apart, on one XCD.
   const int xcd = blockIdx.x & 7, k8 = blockIdx.x >> 3;
   const int w = (k8 / p.row_groups) * 8 + xcd, rg = k8 % p.row_groups;
   if (w >= p.nwaves) return;
   const Cut cut = cut_of(p, lane);
+  if (blockIdx.x == 0) store_cut(p, cut, lane);
   if ((long)w * cut.span >= cut.total) return;
   int pos = w * cut.span;
   const int end = min(pos + cut.span, cut.total);
@@ -608,18 +633,21 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves
     for (int i = 0; i < RB; i++) {
       const int r = (rg * RB + i) * 16 + n;
       const bf16_t *row = nullptr;
-      blk[i].limit = n_ctx;
+      int limit = n_ctx;
       if (r < rows) {
         const int s = c * p.C + r / per, rr = r % per;
         row = static_cast<const bf16_t *>(p.q) + ((((size_t)s * p.L + l) * p.Hkv + h) * per + rr) * D;
-        if (p.nq > 1) blk[i].limit = (int)min((long)n_ctx, (long)n_ctx + own_len(p, s) - (p.nq - 1 - rr % p.nq));
+        if (p.nq > 1) limit = (int)min((long)n_ctx, (long)n_ctx + own_len(p, s) - (p.nq - 1 - rr % p.nq));
       }
       load_queries<D, NG>(blk[i], p, row, lane);
       clear<D, NG>(blk[i]);
-      int m = blk[i].limit;
+      if (RB <= 2) blk[i].limit = limit;
+      else limits[16 * i + n] = limit;
+      if (p.nq > 1) {
 #pragma unroll
-      for (int x = 8; x >= 1; x >>= 1) m = min(m, shfl_xor(m, x));
-      least = min(least, uniform(m));
+        for (int x = 8; x >= 1; x >>= 1) limit = min(limit, shfl_xor(limit, x));
+        least = min(least, uniform(limit));
+      }
     }
     // The queries' loads are done, so that the waits below count tiles alone
     // (and with them the first tiles', which were issued before).
@@ -630,13 +658,13 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves
       wait_lds();  // the slot's tile has been read
       load_tile<D, NG>(ring + next * SLOT, base + (size_t)tn * Q::BYTES, tn < last, lane);
       wait_vm<LOADS *(DEPTH - 1)>();
-      tile_step<D, NG, RB>(blk, ring + at_slot * SLOT, t * Q::KEYS, n_ctx, (t + 1) * Q::KEYS > least, lane);
+      tile_step<D, NG, RB>(blk, ring + at_slot * SLOT, t * Q::KEYS, n_ctx, (t + 1) * Q::KEYS > least, t == tile, limits, lane);
       at_slot = at_slot + 1 == DEPTH ? 0 : at_slot + 1;
     }
     wait_vm<0>();  // the zeros behind the last tile, before the ring starts again
     wait_lds();
     // The records of this piece.
-    float *rec = p.ws + ((size_t)w + (size_t)c * lh + u) * rows * kRecFloats<D>;
+    float *rec = records(p) + ((size_t)w + (size_t)c * lh + u) * rows * kRecFloats<D>;
 #pragma unroll
     for (int i = 0; i < RB; i++) {
 #pragma unroll
@@ -650,7 +678,7 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves
         for (int k = 0; k < NG; k++) off_j[k] = __shfl(blk[i].z[j], (lane & 48) + k, kWave);
         if (r < rows) {
           float *to = rec + (size_t)r * kRecFloats<D>;
-          if (n == 0) *reinterpret_cast<float2_t *>(to) = (float2_t){den > 0.f || den != den ? ref : kNegInf, den};
+          if (n == 0) *reinterpret_cast<float2_t *>(to) = (float2_t){den == 0.f ? kNegInf : ref, den};
 #pragma unroll
           for (int x = 0; x < D / 32; x++) {
             const float o = off_j[x * 32 / Q::GROUP];
@@ -682,49 +710,91 @@ struct OwnChunk {
   uint32_t v[8][D / 32];
 };
 
-template <int D>
 __device__ __forceinline__ int slot_key(int g, int e) { return e < 4 ? 4 * g + e : 16 + 4 * g + e - 4; }
 
+// The own rows of a unit and the query rows r0 .. r0 + nrow - 1 of its
+// sequence. Rows before `first` are in the cache, the new ones after it in the
+// caller's array (another workgroup may be storing them). Both are read as
+// buffers that end with them, so rows past the last live one are zeros,
+// whatever their slots hold.
+struct OwnUnit {
+  const bf16_t *k, *v, *fk, *fv;
+  int u, first, nq, r0, nrow;
+  float sl2;
+};
+
 template <int D>
-__device__ __forceinline__ void load_own(OwnChunk<D> &c, const OwnRows<bf16_t> &K, const OwnRows<bf16_t> &V, int key0, int u,
-                                         int lane) {
+__device__ __forceinline__ OwnUnit own_unit(const QuantAttnParams &p, int unit, int u, int r0, int nrow) {
+  const size_t own0 = (size_t)unit * p.ocap * D, new0 = (size_t)unit * p.nq * D;
+  return OwnUnit{static_cast<const bf16_t *>(p.ok) + own0, static_cast<const bf16_t *>(p.ov) + own0,
+                 static_cast<const bf16_t *>(p.k_new) + new0, static_cast<const bf16_t *>(p.v_new) + new0,
+                 u, p.k_new ? u - p.nq : u, p.nq, r0, nrow, p.scale * kLog2e};
+}
+
+// The rows of a chunk that are in the cache; the bounds check takes the whole
+// offset, so a chunk's place goes into the base.
+template <int D>
+__device__ __forceinline__ rsrc_t held_rows(const bf16_t *rows, const OwnUnit &w, int key0) {
+  return make_rsrc(rows + (size_t)key0 * D, (uint32_t)max(w.first - key0, 0) * (2 * D));
+}
+
+template <int D>
+__device__ __forceinline__ void load_keys(OwnChunk<D> &c, const OwnUnit &w, int key0, int lane) {
+  constexpr int ROW = 2 * D;
   const int n = lane & 15, g = lane >> 4;
+  const rsrc_t held = held_rows<D>(w.k, w, key0);
 #pragma unroll
-  for (int t = 0; t < 2; t++) {
-    const bf16_t *row = K.row(min(key0 + 16 * t + n, u - 1), D);
+  for (int t = 0; t < 2; t++)
 #pragma unroll
-    for (int i = 0; i < D / 32; i++) c.k[t][i] = *reinterpret_cast<const u32x4 *>(row + 32 * i + 8 * g);
-  }
+    for (int i = 0; i < D / 32; i++)
+      c.k[t][i] = __builtin_amdgcn_raw_buffer_load_b128(held, n * ROW + g * 16 + t * 16 * ROW + i * 64, 0, kStreamLoad);
+  if (key0 + 32 > w.first && w.first < w.u) {
+    // New rows; those before the first get an offset past the end.
+    const rsrc_t fresh = make_rsrc(w.fk, w.nq * ROW);
 #pragma unroll
-  for (int e = 0; e < 8; e++) {
-    const bf16_t *row = V.row(min(key0 + slot_key<D>(g, e), u - 1), D) + n * (D / 16);
-    if constexpr (D == 128) {
-      const u32x4 x = *reinterpret_cast<const u32x4 *>(row);
+    for (int t = 0; t < 2; t++) {
+      const uint32_t off = (uint32_t)((key0 + 16 * t + n - w.first) * ROW);
 #pragma unroll
-      for (int i = 0; i < 4; i++) c.v[e][i] = x[i];
-    } else {
-      const u32x2 x = *reinterpret_cast<const u32x2 *>(row);
-      c.v[e][0] = x[0];
-      c.v[e][1] = x[1];
+      for (int i = 0; i < D / 32; i++)
+        c.k[t][i] |= __builtin_amdgcn_raw_buffer_load_b128(fresh, off + (g * 16 + i * 64), 0, kStreamLoad);
     }
   }
 }
 
-// A context's tiles and those before it.
-struct Place {
-  int tiles, before;
-};
-__device__ __forceinline__ Place place_of(const QuantAttnParams &p, const Cut &cut, int c, int lane) {
-  int t = cut.first, sc = cut.sum, before = 0, c0 = 0;
-  for (; c0 + kWave <= c; c0 += kWave) {
-    before += uniform(__shfl(sc, kWave - 1, kWave));
-    t = ctx_tiles(p, c0 + kWave + lane);
-    sc = scan_lanes(t, lane);
+template <int D>
+__device__ __forceinline__ void load_values(OwnChunk<D> &c, const OwnUnit &w, int key0, int lane) {
+  constexpr int ROW = 2 * D;
+  const int n = lane & 15, g = lane >> 4;
+  auto get = [&](rsrc_t r, uint32_t off, uint32_t (&x)[D / 32], bool add) {
+    if constexpr (D == 128) {
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, off + n * 16, 0, kStreamLoad);
+#pragma unroll
+      for (int i = 0; i < 4; i++) x[i] = add ? x[i] | v[i] : v[i];
+    } else {
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, off + n * 8, 0, kStreamLoad);
+#pragma unroll
+      for (int i = 0; i < 2; i++) x[i] = add ? x[i] | v[i] : v[i];
+    }
+  };
+  const rsrc_t held = held_rows<D>(w.v, w, key0);
+#pragma unroll
+  for (int e = 0; e < 8; e++) get(held, slot_key(g, e) * ROW, c.v[e], false);
+  if (key0 + 32 > w.first && w.first < w.u) {
+    const rsrc_t fresh = make_rsrc(w.fv, w.nq * ROW);
+#pragma unroll
+    for (int e = 0; e < 8; e++) get(fresh, (uint32_t)((key0 + slot_key(g, e) - w.first) * ROW), c.v[e], true);
   }
-  Place h;
-  h.tiles = uniform(__shfl(t, c - c0, kWave));
-  h.before = before + uniform(__shfl(sc - t, c - c0, kWave));
-  return h;
+}
+
+// The records of a unit (context c, unit u of it) by waves w0 .. w1 of the context kernel.
+struct Records {
+  int w0, w1;
+};
+__device__ __forceinline__ Records records_of(const QuantAttnParams &p, int c, int u) {
+  const int *cut = reinterpret_cast<const int *>(p.ws);
+  const int span = uniform(cut[0]), before = uniform(cut[1 + c]), tiles = uniform(ctx_tiles(p, c));
+  const int first = before * p.L * p.Hkv + u * tiles;
+  return Records{first / span, tiles > 0 ? (first + tiles - 1) / span : first / span - 1};
 }
 
 // What a wave has of the own rows: 16 query rows (lane's row: n), running
@@ -736,22 +806,6 @@ struct OwnState {
   float m, den;
   float4_t o[D / 16];
 };
-
-// The own rows of a unit and the query rows r0 .. r0 + nrow - 1 of its sequence.
-struct OwnUnit {
-  OwnRows<bf16_t> k, v;
-  int u, nq, r0, nrow;
-  float sl2;
-};
-
-template <int D>
-__device__ __forceinline__ OwnUnit own_unit(const QuantAttnParams &p, int unit, int u, int r0, int nrow) {
-  const size_t own0 = (size_t)unit * p.ocap * D, new0 = (size_t)unit * p.nq * D;
-  const bf16_t *fk = static_cast<const bf16_t *>(p.k_new), *fv = static_cast<const bf16_t *>(p.v_new);
-  return OwnUnit{{static_cast<const bf16_t *>(p.ok) + own0, fk ? fk + new0 : nullptr, u - p.nq},
-                 {static_cast<const bf16_t *>(p.ov) + own0, fv ? fv + new0 : nullptr, u - p.nq},
-                 u, p.nq, r0, nrow, p.scale * kLog2e};
-}
 
 template <int D>
 __device__ __forceinline__ void own_begin(OwnState<D> &st, const QuantAttnParams &p, const OwnUnit &w, int unit, int lane) {
@@ -776,10 +830,10 @@ __device__ __forceinline__ u32x4 value_operand(const uint32_t (&v)[8][D / 32], i
   return w;
 }
 
-// One chunk. p is split into two bfloat16 terms, so that its rounding (2^-17)
-// stays out of the result.
+// One chunk at key0; `next` follows it.
 template <int D>
-__device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const OwnUnit &w, int key0, int lane) {
+__device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const OwnUnit &w, int key0, int next,
+                                         int lane) {
   const int g = lane >> 4;
   float x[2][4], top = kNegInf;
 #pragma unroll
@@ -793,6 +847,7 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
       top = fmaxf(top, x[t][j]);
     }
   }
+  if (next < w.u) load_keys<D>(ch, w, next, lane);
   top = fmaxf(top, shfl_xor(top, 16));
   top = fmaxf(top, shfl_xor(top, 32));
   const float mn = fmaxf(st.m, top), ref = mn == kNegInf ? 0.f : mn;
@@ -818,22 +873,21 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
       hi[2 * t + j / 2] = h;
       lo[2 * t + j / 2] = pack_bf16x2(e0 - bf16_lo(h), e1 - bf16_hi(h));
     }
-  // Rows past the last live one hold anything; so may rows that only later
-  // queries see, where a value that is not finite would reach the others as 0
-  // times it: those get a product per query token.
+  // Rows that only later queries see may hold a value that is not finite, which
+  // would reach the others as 0 times it: those get a product per query token.
   const int sees_all = w.u - (w.nq - 1);
   bool split = false;
-  if (key0 + 32 > sees_all) {
+  if (key0 + 32 > sees_all && w.nq > 1) {
     bool odd = false;
 #pragma unroll
     for (int e = 0; e < 8; e++) {
-      const int key = key0 + slot_key<D>(g, e);
+      bool any = false;
 #pragma unroll
       for (int i = 0; i < D / 32; i++) {
-        if (key >= w.u) ch.v[e][i] = 0u;
         const uint32_t v = ch.v[e][i];
-        odd |= key >= sees_all && ((v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u);
+        any |= (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
       }
+      odd |= any && key0 + slot_key(g, e) >= sees_all;
     }
     split = __any(odd);
   }
@@ -843,6 +897,7 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
       const u32x4 v = value_operand<D>(ch.v, b);
       st.o[b] = mfma_bf16(lo, v, mfma_bf16(hi, v, st.o[b]));
     }
+    if (next < w.u) load_values<D>(ch, w, next, lane);
     return;
   }
 #pragma unroll 1
@@ -851,7 +906,7 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
     uint32_t see[4];
 #pragma unroll
     for (int r = 0; r < 4; r++) {
-      const int k0 = key0 + slot_key<D>(g, 2 * r);
+      const int k0 = key0 + slot_key(g, 2 * r);
       see[r] = (k0 < lim ? 0xffffu : 0u) | (k0 + 1 < lim ? 0xffff0000u : 0u);
     }
 #pragma unroll
@@ -864,6 +919,17 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
       for (int j = 0; j < 4; j++) st.o[b][j] = (w.r0 + 4 * g + j) % w.nq == t ? acc[j] : st.o[b][j];
     }
   }
+  if (next < w.u) load_values<D>(ch, w, next, lane);
+}
+
+// The chunks key0, key0 + stride, .. of a unit. A chunk's keys make way for the
+// next one's once they are multiplied, its values likewise, so that those are
+// under way meanwhile. p is split into two bfloat16 terms, so that its rounding
+// (2^-17) stays out of the result.
+template <int D>
+__device__ __forceinline__ void own_attend(OwnState<D> &st, OwnChunk<D> &ch, const OwnUnit &w, int key0, int stride,
+                                           int lane) {
+  for (; key0 < w.u; key0 += stride) own_step<D>(st, ch, w, key0, key0 + stride, lane);
 }
 
 // Joins (mr, lr, values x whose sum of weights is lr after the factor scale) to a row's (m, den, o).
@@ -899,7 +965,7 @@ __device__ __forceinline__ void put_row(bf16_t *row, int sub, const float (&o)[E
 // its rows attends to the own rows, 32 keys at a time, and joins the context's
 // records as it holds its result: 16 lanes per row, four rows per lane.
 template <int D, int NG>
-__global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(JW))) void quant_join_wave(QuantAttnParams p) {
+__global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(2))) void quant_join_wave(QuantAttnParams p) {
   constexpr int EL = D / 16;
   const int per = p.nq * p.G, blocks = (per + 15) / 16;
   const int unit = blockIdx.x / blocks, r0 = blockIdx.x % blocks * 16;
@@ -914,22 +980,17 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(JW))) voi
   const OwnUnit w = own_unit<D>(p, unit, u, r0, nrow);
   OwnChunk<D> ch;
   if (u > 0) {
-    load_own<D>(ch, w.k, w.v, 0, u, lane);
+    load_keys<D>(ch, w, 0, lane);
+    load_values<D>(ch, w, 0, lane);
     own_begin<D>(st, p, w, unit, lane);
   }
-  const Cut cut = cut_of(p, lane);
-  const Place here = place_of(p, cut, c, lane);
-  for (int key0 = 0; key0 < u; key0 += 32) {
-    if (key0) load_own<D>(ch, w.k, w.v, key0, u, lane);
-    own_step<D>(st, ch, w, key0, lane);
-  }
+  const Records here = records_of(p, c, unit % lh);
+  own_attend<D>(st, ch, w, 0, 32, lane);
   if (p.ok && r0 == 0) store_new<bf16_t, D, kWave>(p, unit, s, u);
   st.den += shfl_xor(st.den, 16);
   st.den += shfl_xor(st.den, 32);
-  const int first = here.before * lh + unit % lh * here.tiles;
-  const int w0 = first / cut.span, w1 = here.tiles > 0 ? (first + here.tiles - 1) / cut.span : w0 - 1;
   const int rows = p.C * per;
-  const float *rec = p.ws + (((size_t)w0 + (size_t)c * lh + unit % lh) * rows + (s % p.C * per + r0)) * kRecFloats<D>;
+  const float *rec = records(p) + (((size_t)here.w0 + (size_t)c * lh + unit % lh) * rows + (s % p.C * per + r0)) * kRecFloats<D>;
   float m[4], den[4], o[4][EL];
 #pragma unroll
   for (int j = 0; j < 4; j++) {
@@ -938,7 +999,7 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(JW))) voi
 #pragma unroll
     for (int e = 0; e < EL; e++) o[j][e] = st.o[e][j];
   }
-  for (int k = w0; k <= w1; k++, rec += (size_t)rows * kRecFloats<D>) {
+  for (int k = here.w0; k <= here.w1; k++, rec += (size_t)rows * kRecFloats<D>) {
 #pragma unroll
     for (int j = 0; j < 4; j++) {
       const float *r = rec + (size_t)min(4 * g + j, nrow - 1) * kRecFloats<D>;
@@ -972,20 +1033,20 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, n = lane & 15, g = lane >> 4;
   const int u = uniform(own_len(p, s));
   const int nrow = min(p.rpw, per - r0);
+
+  const OwnUnit w = own_unit<D>(p, unit, u, r0, nrow);
+  OwnState<D> st;
+  OwnChunk<D> ch;
+  if (u > 0) {
+    load_keys<D>(ch, w, wave * 32, lane);
+    load_values<D>(ch, w, wave * 32, lane);
+    own_begin<D>(st, p, w, unit, lane);
+  }
+  const Records here = records_of(p, c, unit % lh);
   if (p.ok && r0 == 0) store_new<bf16_t, D, NT>(p, unit, s, u);
 
-  const Cut cut = cut_of(p, lane);
-  const Place here = place_of(p, cut, c, lane);
-
   if (u > 0) {
-    const OwnUnit w = own_unit<D>(p, unit, u, r0, nrow);
-    OwnState<D> st;
-    own_begin<D>(st, p, w, unit, lane);
-    for (int key0 = wave * 32; key0 < u; key0 += kOwnWaves * 32) {
-      OwnChunk<D> ch;
-      load_own<D>(ch, w.k, w.v, key0, u, lane);
-      own_step<D>(st, ch, w, key0, lane);
-    }
+    own_attend<D>(st, ch, w, wave * 32, kOwnWaves * 32, lane);
     st.den += shfl_xor(st.den, 16);
     st.den += shfl_xor(st.den, 32);
     if (g == 0) {
@@ -1017,13 +1078,11 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
         fold<EL>(m, den, o, wm[w][row], wl[w][row], 1.f, x);
       }
     }
-    if (here.tiles > 0) {
-      const int first = here.before * lh + unit % lh * here.tiles;
-      const int w0 = first / cut.span, w1 = (first + here.tiles - 1) / cut.span;
+    {
       const int rows = p.C * per, r = s % p.C * per + r0 + row;
-      const float *rec = p.ws + (((size_t)(w0 + part) + (size_t)c * lh + unit % lh) * rows + r) * kRecFloats<D>;
+      const float *rec = records(p) + (((size_t)(here.w0 + part) + (size_t)c * lh + unit % lh) * rows + r) * kRecFloats<D>;
 #pragma unroll 4
-      for (int k = w0 + part; k <= w1; k += parts, rec += (size_t)parts * rows * kRecFloats<D>) {
+      for (int k = here.w0 + part; k <= here.w1; k += parts, rec += (size_t)parts * rows * kRecFloats<D>) {
         const float2_t ml = *reinterpret_cast<const float2_t *>(rec);
         float x[EL];
         record_values<EL>(rec, sub, x);
@@ -1065,7 +1124,7 @@ void plan(QuantAttnParams *p) {
   p->row_groups = (blocks + kMaxBlocks - 1) / kMaxBlocks;
   p->rb = (blocks + p->row_groups - 1) / p->row_groups;
   const double tiles = (double)p->P * p->L * p->Hkv * p->ntiles;
-  const int waves = kChipSimds * (p->rb == 1 ? kCtxWaves<1> : p->rb <= 3 ? kCtxWaves<3> : kCtxWaves<4>);
+  const int waves = kChipSimds * (p->rb <= 3 ? kCtxWaves<3> : kCtxWaves<4>);
   const int most = waves / p->row_groups > 64 ? waves / p->row_groups : 64;
   p->min_span = kMinSpan;
   const double want = tiles / kMinSpan + 1;
@@ -1118,7 +1177,7 @@ size_t quant_attn_workspace_bytes(const QuantAttnParams &params) {
   plan(&p);
   // A wave's piece of a unit has record wave + unit.
   const size_t pieces = (size_t)p.nwaves + (size_t)p.P * p.L * p.Hkv;
-  return pieces * p.C * p.nq * p.G * (4 + p.D / 2) * sizeof(float);
+  return (cut_floats(p.P) + pieces * p.C * p.nq * p.G * (4 + p.D / 2)) * sizeof(float);
 }
 
 hipError_t launch_quant_attn(const QuantAttnParams &params, hipStream_t stream) {
