@@ -25,7 +25,7 @@ namespace kvr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMergeWaves = 8;
+constexpr int kMergeWaves = 16;
 constexpr int kListMax = 1024;  // splits * top_k bound of a row's merge
 
 // Row r of the call: the S (T + 1) target rows, then the S T draft rows.
@@ -54,9 +54,143 @@ __device__ __forceinline__ uint64_t *list_at(const VerifyParams &p, int r, int s
   return p.ws + ((size_t)r * p.splits + split) * kmax;
 }
 
-// One split of a row: its top_k keys, in any order, zeros after them.
+// The top_k best keys of a workgroup's wave buffers, sorted, zeros after them.
+template <int NW>
+__device__ __forceinline__ void write_best(Cands &cs, uint64_t *cand, int *cand_n, int K, int lane, int wave,
+                                           uint64_t *keys) {
+  __shared__ uint64_t best[kTopKMax];
+  if (cs.cnt > K) cand_reduce_any(cs, K, K, lane);
+  if (lane == 0) cand_n[wave] = cs.cnt;
+  __syncthreads();
+  if (wave != 0) return;
+  int off[NW + 1];
+  off[0] = 0;
+#pragma unroll
+  for (int w = 0; w < NW; w++) off[w + 1] = off[w] + cand_n[w];
+  const int n = gather_select<NW * kTopKMax / kWave, NW>(cand, off, K, lane, best);
+  wave_lds_sync();
+  const uint64_t key = lane < n ? best[lane] : 0;
+  int rank = 0;
+  for (int j = 0; j < n; j++) rank += best[j] > key;
+  if (lane < n) keys[rank] = key;
+  else if (lane < K) keys[lane] = 0;
+}
+
+constexpr int kU = 10;                        // vectors of eight logits per thread
+constexpr int kRoundVecs = kThreads * kU;
+
+// One split of a row, all of its logits in registers at once: its top_k keys,
+// sorted, zeros after them. The top_k-th largest of the 256 lanes' maxima (16
+// leading bits of it) bounds the split's top_k-th best from below, so about
+// top_k logits are candidates and most vectors are passed over by one compare;
+// they are ranked by counting. Where they outnumber the threads (many equal
+// logits) or too few lanes hold a logit for a bound, the waves' buffers take
+// them, from the same registers.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_split(VerifyParams p) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 5 : 4))) void verify_split(VerifyParams p) {
+  constexpr int U = kU, NT = kThreads, NW = NT / kWave;
+  __shared__ uint32_t lane_max[NT];
+  __shared__ __align__(16) uint64_t cand[NW * kCandCap];
+  __shared__ int count, cand_n[NW];
+  static_assert(NW * kCandCap >= NT && NT % 8 == 0, "a candidate per thread, ranked in eights");
+  const int split = blockIdx.x % p.splits, r = blockIdx.x / p.splits;
+  const Row row = row_of(p, r, sizeof(T));
+  if (!row.live) return;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, K = row.top_k;
+  const T *x = reinterpret_cast<const T *>(row.x);
+  // Vectors from the row's first 16-byte boundary, element `skip`; the logits
+  // before it and the last few one per thread of the last split's first wave.
+  const int skip = min((int)((0 - reinterpret_cast<uintptr_t>(x)) % 16 / sizeof(T)), row.V);
+  const int nvec = (row.V - skip) / 8, per = (nvec + p.splits - 1) / p.splits;
+  const int v0 = min(split * per, nvec), v1 = min(v0 + per, nvec);
+  const rsrc_t rr = row_rsrc(x + skip, (uint32_t)v1 * 8u * (uint32_t)sizeof(T));
+  Vec8<T> w[U];
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    w[u].load(rr, v0 + tid + u * NT);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (tid == 0) count = 0;
+  cand[tid] = 0;
+  float lm[U], mx = kNegInf;
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    float a[8];
+    w[u].get(a);
+    lm[u] = kNegInf;
+    if (v0 + tid + u * NT < v1) {
+#pragma unroll
+      for (int e = 0; e < 8; e++) lm[u] = fmaxf(lm[u], a[e]);  // a NaN is passed over
+    }
+    mx = fmaxf(mx, lm[u]);
+  }
+  const int et = tid < skip ? tid : nvec * 8 + tid;
+  const bool has_tail = split == p.splits - 1 && et < row.V && tid < kWave;
+  const float tail = has_tail ? load1(x + et) : kNegInf;
+  mx = fmaxf(mx, tail);
+  lane_max[tid] = order_bits(mx);
+  __syncthreads();
+
+  const float vmin = group_bound<NW>(lane_max, lane, K);  // nothing below it is among the split's best
+  bool over = vmin == kNegInf;
+  if (over) count = NT + 1;
+  auto offer = [&](float v, uint32_t id) {
+    const int at = atomicAdd(&count, 1);
+    if (at < NT) cand[at] = cand_key(v, id);
+    over = at >= NT;
+  };
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    const int v = v0 + tid + u * NT;
+    if (v < v1 && !over && lm[u] >= vmin) {
+      float a[8];
+      w[u].get(a);
+#pragma unroll
+      for (int e = 0; e < 8; e++)
+        if (!over && a[e] >= vmin) offer(a[e], (uint32_t)(skip + v * 8 + e));
+    }
+  }
+  if (has_tail && !over && tail >= vmin) offer(tail, (uint32_t)et);
+  __syncthreads();
+
+  uint64_t *keys = list_at(p, r, split);
+  const int n = count;
+  if (n <= NT) {
+    // Counting gives the same order whatever the order of the atomics.
+    const uint64_t key = tid < n ? cand[tid] : 0;
+    int rank = 0;
+    for (int j = 0; j < n; j += 8)
+#pragma unroll
+      for (int q = 0; q < 8; q++) rank += cand[j + q] > key;  // zeros past the last
+    if (tid < n) {
+      if (rank < K) keys[rank] = key;
+    } else if (tid < K) {
+      keys[tid] = 0;
+    }
+    return;
+  }
+  Cands cs{cand + wave * kCandCap, 0, 1, kNegInf};
+  __syncthreads();  // every thread is past its read of the count and the candidates
+  cand_seed(cs, mx, K);
+#pragma unroll 1
+  for (int u = 0; u < U; u++) {
+    float a[8];
+    Vec8<T> wu = w[0];
+#pragma unroll
+    for (int q = 1; q < U; q++)
+      if (q == u) wu = w[q];
+    wu.get(a);
+    const int v = v0 + tid + u * NT;
+    cand_offer(cs, K, lane, a, (uint32_t)(skip + v * 8), v < v1 ? 8 : 0);
+  }
+  float a[8] = {tail, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf};
+  if (wave == 0) cand_offer(cs, K, lane, a, (uint32_t)et, has_tail ? 1 : 0);
+  write_best<NW>(cs, cand, cand_n, K, lane, wave, keys);
+}
+
+// One split of a row of more logits than that, streamed.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void verify_stream(VerifyParams p) {
   constexpr int NW = kThreads / kWave;
   __shared__ uint64_t cand[NW * kCandCap];
   __shared__ int cand_n[NW];
@@ -66,7 +200,7 @@ __global__ __launch_bounds__(kThreads) void verify_split(VerifyParams p) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, K = row.top_k;
   const T *x = reinterpret_cast<const T *>(row.x);
   const int per = (row.V + p.splits - 1) / p.splits;
-  const int e0 = min(split * per, row.V), e1 = min(e0 + per, row.V);
+  const int e0 = min((long)split * per, (long)row.V), e1 = min((long)e0 + per, (long)row.V);
   Cands cs{cand + wave * kCandCap, 0, 1, kNegInf};
   for (int eb = e0; eb < e1; eb += kThreads) {
     float a[8] = {kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf, kNegInf};
@@ -74,17 +208,7 @@ __global__ __launch_bounds__(kThreads) void verify_split(VerifyParams p) {
     if (has) a[0] = load1(x + eb + tid);
     cand_offer(cs, K, lane, a, (uint32_t)(eb + tid), has ? 1 : 0);
   }
-  if (cs.cnt > K) cand_reduce_any(cs, K, K, lane);
-  if (lane == 0) cand_n[wave] = cs.cnt;
-  __syncthreads();
-  if (wave != 0) return;
-  int off[NW + 1];
-  off[0] = 0;
-#pragma unroll
-  for (int w = 0; w < NW; w++) off[w + 1] = off[w] + cand_n[w];
-  uint64_t *keys = list_at(p, r, split);
-  const int nk = gather_select<NW * kTopKMax / kWave, NW>(cand, off, K, lane, keys);
-  for (int q = nk + lane; q < K; q += kWave) keys[q] = 0;
+  write_best<NW>(cs, cand, cand_n, K, lane, wave, list_at(p, r, split));
 }
 
 // A distribution as a list: lane i holds token i, by falling probability.
@@ -93,20 +217,31 @@ struct Dist {
   double p;
 };
 
-// The k best keys of the row's splits, sorted over the lanes, by one wave.
+// The k best keys of the row's splits, sorted over the lanes, by one wave. The
+// largest of the splits' k-th keys bounds the row's k-th from below (the split
+// that has it has k); what reaches it is ranked by counting, after a bitwise
+// search for the k-th key where that is more than a wave's lanes.
+template <int NPL>
 __device__ __forceinline__ uint64_t merge_keys(const VerifyParams &p, int r, int k, int lane, uint64_t *tmp) {
-  constexpr int NPL = kListMax / kWave;
   const uint64_t *src = list_at(p, r, 0);
-  const int kmax = max(p.top_k, p.top_kd);
+  const int kmax = max(p.top_k, p.top_kd), all = p.splits * k;
   uint64_t v[NPL];
 #pragma unroll
   for (int i = 0; i < NPL; i++) {
-    const int e = lane + i * kWave, split = e / k;
-    v[i] = split < p.splits ? src[(size_t)split * kmax + e % k] : 0;
+    const int e = lane + i * kWave;
+    v[i] = e < all ? src[(size_t)(e / k) * kmax + e % k] : 0;
   }
-  const uint64_t thr = select_threshold<NPL>(v, k, k);
+  uint64_t bound = 1;
+#pragma unroll
+  for (int i = 0; i < NPL; i++) {
+    const int e = lane + i * kWave;
+    if (e < all && e % k == k - 1) bound = max(bound, v[i]);
+  }
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) bound = max(bound, (uint64_t)__shfl_xor((unsigned long long)bound, m, kWave));
+  if (wave_count_ge<NPL>(v, bound) > kWave) bound = select_threshold<NPL>(v, k, kWave);
   wave_lds_sync();
-  const int n = wave_store_ge<NPL>(tmp, v, thr, lane);
+  const int n = wave_store_ge<NPL>(tmp, v, bound, lane);
   wave_lds_sync();
   const uint64_t key = lane < n ? tmp[lane] : 0;
   int rank = 0;
@@ -114,7 +249,7 @@ __device__ __forceinline__ uint64_t merge_keys(const VerifyParams &p, int r, int
   wave_lds_sync();
   if (lane < n) tmp[rank] = key;
   wave_lds_sync();
-  return lane < n ? tmp[lane] : 0;
+  return lane < n && lane < k ? tmp[lane] : 0;
 }
 
 __device__ __forceinline__ double lane_cumsum(double x, int lane) {
@@ -141,8 +276,12 @@ __device__ __forceinline__ Dist distribution(uint64_t key, double temp, double t
   return Dist{live && lane < keep ? (int)~(uint32_t)(key & 0xffffffffu) : -1, w / mass};
 }
 
+// The lists of a sequence's rows, a wave per row; then one wave goes through the
+// positions. NPL: keys per lane of a merge.
+template <int NPL>
 __global__ __launch_bounds__(kMergeWaves * kWave) void verify_walk(VerifyParams p) {
   extern __shared__ char lds[];
+  __shared__ int stands[kWave];  // T is at most 32
   const int s = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int nd = p.n_draft ? min(max(p.n_draft[s], 0), p.T) : p.T;
   // Probabilities and ids of the target's rows, then of the draft's; scratch of the merges.
@@ -155,43 +294,46 @@ __global__ __launch_bounds__(kMergeWaves * kWave) void verify_walk(VerifyParams 
     const bool draft = i > nd;
     const int t = draft ? i - nd - 1 : i;
     const int r = draft ? p.S * (p.T + 1) + s * p.T + t : s * (p.T + 1) + t;
-    const uint64_t key = merge_keys(p, r, draft ? p.top_kd : p.top_k, lane, tmp);
+    const uint64_t key = merge_keys<NPL>(p, r, draft ? p.top_kd : p.top_k, lane, tmp);
     const Dist d = distribution(key, draft ? p.tempd : p.temp, draft ? p.top_pd : p.top_p, lane);
     const int at = (draft ? p.T + 1 + t : t) * kWave + lane;
     prob[at] = d.p;
     ids[at] = d.id;
   }
   __syncthreads();
+  // Which of the drafted tokens would stand by themselves, a wave per position.
+  for (int t = wave; t < nd; t += kMergeWaves) {
+    const int tok = p.tok[(size_t)s * p.T + t];
+    const float ua = p.u_accept[(size_t)s * p.T + t];
+    const uint64_t ip = __ballot(ids[t * kWave + lane] == tok && tok >= 0);
+    const double px = ip ? prob[t * kWave + __ffsll((long long)ip) - 1] : 0.0;
+    double qx = 1.0;
+    if (p.draft) {
+      const uint64_t iq = __ballot(ids[(p.T + 1 + t) * kWave + lane] == tok && tok >= 0);
+      qx = iq ? prob[(p.T + 1 + t) * kWave + __ffsll((long long)iq) - 1] : 0.0;
+    }
+    if (lane == 0) stands[t] = (double)ua * qx < px;
+  }
+  __syncthreads();
   if (wave != 0) return;
   int32_t *out = p.tokens + (size_t)s * (p.T + 1);
-  int acc = 0;
+  const uint64_t fell = __ballot(lane < nd && !stands[lane]);
+  const int acc = fell ? __ffsll((long long)fell) - 1 : nd;
   double r = 0.0;
-  for (; acc < nd; acc++) {
-    const int tok = p.tok[(size_t)s * p.T + acc];
-    const double P = prob[acc * kWave + lane];
-    const int id = ids[acc * kWave + lane];
-    const double Pd = p.draft ? prob[(p.T + 1 + acc) * kWave + lane] : (lane == 0 ? 1.0 : 0.0);
-    const int jd = p.draft ? ids[(p.T + 1 + acc) * kWave + lane] : (lane == 0 ? tok : -1);
-    // The two probabilities of the drafted token: at most one lane of each has it.
-    const uint64_t ip = __ballot(id == tok && id >= 0), iq = __ballot(jd == tok && jd >= 0);
-    const double px = ip ? __shfl(P, __ffsll((long long)ip) - 1, kWave) : 0.0;
-    const double qx = iq ? __shfl(Pd, __ffsll((long long)iq) - 1, kWave) : 0.0;
-    if ((double)p.u_accept[(size_t)s * p.T + acc] * qx < px) {
-      if (lane == 0) out[acc] = tok;
-      continue;
-    }
-    // What the target has beyond the draft.
-    double q = 0.0;
-    for (int j = 0; j < kWave; j++) {
-      const int other = __shfl(jd, j, kWave);
-      const double oq = __shfl(Pd, j, kWave);
-      if (other == id && id >= 0) q = oq;
-    }
-    r = id >= 0 ? fmax(P - q, 0.0) : 0.0;
-    break;
-  }
   const double P = prob[acc * kWave + lane];
   const int id = ids[acc * kWave + lane];
+  if (acc < nd) {
+    // What the target has beyond the draft.
+    double q = 0.0;
+    if (p.draft) {
+      const int at = (p.T + 1 + acc) * kWave, n = __popcll(__ballot(ids[at + lane] >= 0));  // the tokens come first
+      for (int j = 0; j < n; j++)
+        if (ids[at + j] == id) q = prob[at + j];
+    } else if (id == p.tok[(size_t)s * p.T + acc]) {
+      q = 1.0;
+    }
+    r = id >= 0 ? fmax(P - q, 0.0) : 0.0;
+  }
   if (acc == nd || !__any(r > 0.0)) r = P;
   const double cum = lane_cumsum(r, lane);
   const double all = __shfl(cum, kWave - 1, kWave);
@@ -199,20 +341,34 @@ __global__ __launch_bounds__(kMergeWaves * kWave) void verify_walk(VerifyParams 
   const uint64_t any = __ballot(r > 0.0);
   const int pick = over ? __ffsll((long long)over) - 1 : any ? 63 - __clzll((long long)any) : 0;
   const int next = __shfl(id, pick, kWave);
-  for (int t = acc + lane; t <= p.T; t += kWave) out[t] = t == acc ? next : -1;
+  for (int t = lane; t <= p.T; t += kWave) out[t] = t < acc ? p.tok[(size_t)s * p.T + t] : t == acc ? next : -1;
   if (lane == 0) {
     p.accepted[s] = acc;
     if (p.len_out) p.len_out[s] = p.len[s] - (nd - acc);
   }
 }
 
+// Splits of a row: enough that a workgroup holds one at once, where the merge
+// takes that many lists; with few rows more of them, up to 1024 workgroups and
+// four keys per lane of the merge.
 int verify_splits(int S, int T, int V, int Vd, int top_k) {
-  const int rows = S * (2 * T + 1), vmax = V > Vd ? V : Vd;
-  int n = (1024 + rows - 1) / rows;
-  const int most = kListMax / top_k, useful = (vmax + 8191) / 8192;
+  const long rows = (long)S * (2 * T + 1), nvec = (V > Vd ? V : Vd) / 8;
+  long n = (1024 + rows - 1) / rows;
+  const long useful = (nvec + kThreads - 1) / kThreads, round = (nvec + kRoundVecs - 1) / kRoundVecs;
+  const long lists = 4 * kWave / top_k;
+  n = n < lists ? n : lists;
   n = n < useful ? n : useful;
-  n = n < most ? n : most;
-  return n < 1 ? 1 : n;
+  n = n > round ? n : round;
+  n = n < kListMax / top_k ? n : kListMax / top_k;
+  return n < 1 ? 1 : (int)n;
+}
+
+template <typename T>
+void launch_rows(const VerifyParams &p, dim3 grid, hipStream_t stream) {
+  if ((p.V / 8 + p.splits - 1) / p.splits <= kRoundVecs)
+    hipLaunchKernelGGL(verify_split<T>, grid, dim3(kThreads), 0, stream, p);
+  else
+    hipLaunchKernelGGL(verify_stream<T>, grid, dim3(kThreads), 0, stream, p);
 }
 
 }  // namespace
@@ -227,13 +383,15 @@ hipError_t launch_verify_draft(const VerifyParams &params, hipStream_t stream) {
   p.splits = verify_splits(p.S, p.T, p.V, p.Vd, k);
   const int rows = p.S * (p.T + 1) + (p.draft ? p.S * p.T : 0);
   const dim3 grid((uint32_t)rows * p.splits);
-  if (p.dtype == 0) hipLaunchKernelGGL(verify_split<float>, grid, dim3(kThreads), 0, stream, p);
-  else hipLaunchKernelGGL(verify_split<bf16_t>, grid, dim3(kThreads), 0, stream, p);
+  if (p.dtype == 0) launch_rows<float>(p, grid, stream);
+  else launch_rows<bf16_t>(p, grid, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const size_t lds = (size_t)(2 * p.T + 1) * kWave * (sizeof(double) + sizeof(int)) +
                      (size_t)kMergeWaves * kWave * sizeof(uint64_t);
-  hipLaunchKernelGGL(verify_walk, dim3(p.S), dim3(kMergeWaves * kWave), lds, stream, p);
+  const dim3 seqs(p.S), threads(kMergeWaves * kWave);
+  if (p.splits * k <= 4 * kWave) hipLaunchKernelGGL(verify_walk<4>, seqs, threads, lds, stream, p);
+  else hipLaunchKernelGGL(verify_walk<kListMax / kWave>, seqs, threads, lds, stream, p);
   return hipGetLastError();
 }
 
