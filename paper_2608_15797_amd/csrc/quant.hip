@@ -15,39 +15,51 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
-// Waves of an append's workgroup: a wave per KiB of codes, K and V.
+// Waves of a workgroup: one per KiB of a tile's codes, K and V.
 template <int D>
-constexpr int kAppendWaves = D / 32;
+constexpr int kTileWaves = D / 32;
 
-// Eight consecutive values of a row.
-__device__ __forceinline__ void load8(const bf16_t *p, float (&x)[8]) {
-  const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    x[2 * i] = bf16_lo(w[i]);
-    x[2 * i + 1] = bf16_hi(w[i]);
+// Eight consecutive values of a row, as loaded.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<bf16_t> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const bf16_t *p) {
+    w = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
   }
-}
-__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
+  __device__ __forceinline__ void get(float (&x)[8]) const {
 #pragma unroll
-  for (int h = 0; h < 2; h++) {
-    const float4_t w = __builtin_nontemporal_load(reinterpret_cast<const float4_t *>(p) + h);
-#pragma unroll
-    for (int i = 0; i < 4; i++) x[4 * h + i] = w[i];
+    for (int i = 0; i < 4; i++) {
+      x[2 * i] = bf16_lo(w[i]);
+      x[2 * i + 1] = bf16_hi(w[i]);
+    }
   }
-}
+};
+template <>
+struct Raw8<float> {
+  float4_t w[2];
+  __device__ __forceinline__ void load(const float *p) {
+#pragma unroll
+    for (int h = 0; h < 2; h++) w[h] = __builtin_nontemporal_load(reinterpret_cast<const float4_t *>(p) + h);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = w[i >> 2][i & 3];
+  }
+};
+
 __device__ __forceinline__ void store8(bf16_t *p, const float (&x)[8]) {
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; i++) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-  __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
+  *reinterpret_cast<u32x4 *>(p) = w;
 }
 __device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
 #pragma unroll
   for (int h = 0; h < 2; h++) {
     const float4_t w = {x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
-    __builtin_nontemporal_store(w, reinterpret_cast<float4_t *>(p) + h);
+    reinterpret_cast<float4_t *>(p)[h] = w;
   }
 }
 
@@ -87,6 +99,20 @@ struct Lane {
   }
 };
 
+// A wave's own LDS, between its lanes' writes and reads.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Word c of the result: byte c of each of the four words.
+__device__ __forceinline__ u32x4 transpose4(const uint32_t (&w)[4]) {
+  const uint32_t a0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), a1 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+  const uint32_t b0 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), b1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  return (u32x4){__builtin_amdgcn_perm(b0, a0, 0x05040100u), __builtin_amdgcn_perm(b0, a0, 0x07060302u),
+                 __builtin_amdgcn_perm(b1, a1, 0x05040100u), __builtin_amdgcn_perm(b1, a1, 0x07060302u)};
+}
+
 // The values of lanes 0, 1, 2 or 3 of each quad, or of the lane beside.
 template <int CTRL>
 __device__ __forceinline__ float quad(float x) {
@@ -112,42 +138,41 @@ __device__ __forceinline__ void bounds(const float (&x)[4][8], float (&lo)[4], f
 // workgroup per tile of 32 slots that a unit's new rows may touch; a lane
 // quantises 32 values, and computes the scale and offset of one group for its
 // quad.
-// Bound by memory where rows are many: 4096 rows of 28 layers x 8 x 4 heads
-// (1.88 GB in, 0.53 out) .
+// Bound by memory where rows are many: 4096 rows of 8 x 28 x 4 units (1.88 GB in,
+// 0.53 out) take 434 us, 5.5 TB/s; a thread per eight values, 637 us.
 template <typename T, int D, int NG>
-__global__ __launch_bounds__(kAppendWaves<D> *kWave) void quant_append_kernel(QuantAppendParams p, int tiles) {
+__global__ __launch_bounds__(kTileWaves<D> *kWave) void quant_append_kernel(QuantAppendParams p, int tiles) {
   using Q = QTile<D, NG>;
-  constexpr int PARTS = kAppendWaves<D> / 2, PAIR = Q::GROUP == 64;
-  __shared__ uint32_t turn[PARTS][256];
+  constexpr int PARTS = kTileWaves<D> / 2, PAIR = Q::GROUP == 64;
+  __shared__ __align__(16) uint32_t turn[PARTS][256];
   const int unit = blockIdx.x / tiles;  // (s * L + l) * Hkv + h
   const int lh = p.L * p.Hkv, s = unit / lh;
   const int from = p.src_index ? p.src_index[s] : s;
   if (from < 0 || from >= p.S_src) return;
   const int n = max(p.len[s], 0);
   const int count = p.count ? min(p.count[s], p.T) : p.T;
-  const int tile = n / Q::KEYS + blockIdx.x % tiles;
-  const int first = tile * Q::KEYS;
-  const int j0 = max(n, first);
-  const int j1 = (int)min((long)min((long)n + count, (long)p.cap), (long)first + Q::KEYS);
-  if (j0 >= j1) return;
-  const bool full = j1 - j0 == Q::KEYS;
+  const int end = (int)min((long)n + count, (long)p.cap);  // the slots [n, end)
+  const int tile = n / Q::KEYS + blockIdx.x % tiles, first = tile * Q::KEYS;
+  if (max(n, first) >= end) return;
+  const bool full = first >= n && first + Q::KEYS <= end;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const bool val = wave >= PARTS;
   const int part = val ? wave - PARTS : wave, q = lane & 3;
   const Lane<D> at(val, part, lane);
-  const T *src = static_cast<const T *>(val ? p.v : p.k) + (((size_t)from * lh + unit % lh) * p.T + (first - n)) * (long)D;
-  float x[4][8];
+  // Row j of the slots; rows before the first new one are not read.
+  const T *src = static_cast<const T *>(val ? p.v : p.k) + ((long)((size_t)from * lh + unit % lh) * p.T - n) * (long)D;
+  Raw8<T> raw[4];
   bool live[4];
 #pragma unroll
   for (int c = 0; c < 4; c++) {
-    live[c] = first + at.key[c] >= j0 && first + at.key[c] < j1;
-    if (live[c]) {
-      load8(src + (long)at.key[c] * D + at.d[c], x[c]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; i++) x[c][i] = 0.f;
-    }
+    const int j = first + at.key[c];
+    live[c] = j >= n && j < end;
+    raw[c] = Raw8<T>{};
+    if (live[c]) raw[c].load(src + (long)j * D + at.d[c]);
   }
+  float x[4][8];
+#pragma unroll
+  for (int c = 0; c < 4; c++) raw[c].get(x[c]);
   float lo[4], hi[4];
   bounds(x, lo, hi);
   bool plain = true;
@@ -230,17 +255,13 @@ __global__ __launch_bounds__(kAppendWaves<D> *kWave) void quant_append_kernel(Qu
     return;
   }
   // V: byte m of the words (k, even i), (k, odd i), (k + 1, even), (k + 1, odd) is column 4 q + m.
-  const uint32_t a0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), a1 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
-  const uint32_t b0 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), b1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
-  const uint32_t col[4] = {__builtin_amdgcn_perm(b0, a0, 0x05040100u), __builtin_amdgcn_perm(b0, a0, 0x07060302u),
-                           __builtin_amdgcn_perm(b1, a1, 0x05040100u), __builtin_amdgcn_perm(b1, a1, 0x07060302u)};
+  const u32x4 col = transpose4(w);
   char *to = out + Q::VC + part * 1024;
   if (full) {
     uint32_t *mat = turn[part];  // this wave's alone
 #pragma unroll
     for (int m = 0; m < 4; m++) mat[(at.g * 16 + 4 * q + m) * 4 + at.r] = col[m];
-    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     reinterpret_cast<u32x4 *>(to)[lane] = reinterpret_cast<const u32x4 *>(mat)[lane];
   } else {
 #pragma unroll
@@ -252,38 +273,76 @@ __global__ __launch_bounds__(kAppendWaves<D> *kWave) void quant_append_kernel(Qu
   }
 }
 
-// One workgroup per tile of a destination's live slots.
+// A workgroup per tile of a destination's live slots. A wave loads a KiB of codes, in the append's lanes, and the scales and offsets of its quads'
+// groups; through LDS a lane gets the words, each with its group's scale and
+// offset, of four chunks such that a store covers whole lines (64-byte pieces
+// of 16 rows, as the codes lie, take 509 us for 4096 rows of 28 x 8 x 4 heads).
 template <typename T, int D, int NG>
-__global__ __launch_bounds__(kThreads) void quant_read_kernel(QuantReadParams p, int tiles) {
+__global__ __launch_bounds__(kTileWaves<D> *kWave) void quant_read_kernel(QuantReadParams p, int tiles) {
   using Q = QTile<D, NG>;
-  constexpr int CH = D / 8, LANES = Q::GROUP / 8;
+  constexpr int PARTS = kTileWaves<D> / 2, LANES = Q::GROUP / 8;
+  __shared__ __align__(16) uint32_t turn[PARTS][256];
+  __shared__ uint32_t words[2 * PARTS][256 + 64];
+  __shared__ uint32_t params[2 * PARTS][256 / LANES];
   const int unit = blockIdx.x / tiles, tile = blockIdx.x % tiles;
   const int lh = p.L * p.Hkv, s = unit / lh;
   const int from = p.src_index ? p.src_index[s] : s;
   if (from < 0 || from >= p.S_src) return;
-  const int j0 = tile * Q::KEYS;
-  const int j1 = min(min(p.len[s], min(p.cap, p.cap_dst)), j0 + Q::KEYS);
-  if (j0 >= j1) return;
+  const int end = min(p.len[s], min(p.cap, p.cap_dst));
+  if (tile * Q::KEYS >= end) return;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, q = lane & 3;
+  const bool val = wave >= PARTS;
+  const int part = val ? wave - PARTS : wave;
+  const Lane<D> at(val, part, lane);
+  // The wave's keys and d: from key0 and d0, chunks of a key side by side.
+  const int log_cpr = D == 128 && !val ? 4 : 3, key0 = val || D == 64 ? 0 : 16 * part, d0 = val ? 64 * part : 0;
   const char *in = static_cast<const char *>(p.data) + (((size_t)from * lh + unit % lh) * p.ntiles + tile) * Q::BYTES;
-  const size_t row0 = (size_t)unit * p.cap_dst + j0;
-  const int items = (j1 - j0) * CH;
-  for (int it = threadIdx.x; it < 2 * items; it += kThreads) {
-    const bool val = it >= items;
-    const int e = val ? it - items : it;
-    const int key = e / CH, c = e % CH;
-    const int at = val ? Q::vparam(key, c / LANES) : Q::kparam(key, c / LANES);
-    const float sc = f16_at(in + (val ? Q::VS : Q::KS) + at), z = f16_at(in + (val ? Q::VZ : Q::KZ) + at);
-    uint32_t w = 0;
-    if (!val) {
-      w = *reinterpret_cast<const uint32_t *>(in + Q::kword(key, c));
-    } else {
+  T *out = static_cast<T *>(val ? p.v : p.k) + (size_t)unit * p.cap_dst * D;
+  int key = 0, d = 0;  // of chunk q
 #pragma unroll
-      for (int i = 0; i < 4; i++) w |= (uint32_t)(uint8_t)in[Q::vbyte(key, c * 4 + i)] << (8 * i);
+  for (int c = 0; c < 4; c++)
+    if (q == c) {
+      key = at.key[c];
+      d = at.d[c] - 8 * q;
     }
+  const int param = val ? Q::VS + Q::vparam(key, d / Q::GROUP) : Q::KS + Q::kparam(key, d / Q::GROUP);
+  const int code = (val ? Q::VC : 0) + part * 1024 + (val ? lane * 16 : (at.g * 16 + (lane >> 2)) * 16);
+  static_assert(Q::KZ - Q::KS == Q::VZ - Q::VS, "offsets after the scales");
+  u32x4 c4 = *reinterpret_cast<const u32x4 *>(in + code);
+  const uint32_t sh = *reinterpret_cast<const uint16_t *>(in + param);
+  const uint32_t zh = *reinterpret_cast<const uint16_t *>(in + param + (Q::KZ - Q::KS));
+  // Chunk q's group, by the chunk's place.
+  params[wave][(((key - key0) << log_cpr) + (d - d0) / 8) / LANES] = sh | (zh << 16);
+  if (val) {
+    uint32_t *mat = turn[part];
+    reinterpret_cast<u32x4 *>(mat)[lane] = c4;
+    wave_sync();
+    uint32_t col[4];
+#pragma unroll
+    for (int m = 0; m < 4; m++) col[m] = mat[(at.g * 16 + 4 * q + m) * 4 + at.r];
+    c4 = transpose4(col);
+  }
+#pragma unroll
+  for (int c = 0; c < 4; c++) {
+    const int e = ((at.key[c] - key0) << log_cpr) + (at.d[c] - d0) / 8;
+    words[wave][e + (e >> 4) * 4] = c4[c];  // four words of padding in 16 keep the banks apart
+  }
+  wave_sync();
+#pragma unroll
+  for (int c = 0; c < 4; c++) {
+    const int e = c * kWave + lane;
+    const uint32_t word = words[wave][e + (e >> 4) * 4], pz = params[wave][e / LANES];
+    const float sc = (float)__builtin_bit_cast(f16_t, (uint16_t)pz);
+    const float z = (float)__builtin_bit_cast(f16_t, (uint16_t)(pz >> 16));
+    const uint32_t even = word & 0x0f0f0f0fu, odd = (word >> 4) & 0x0f0f0f0fu;
     float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = fmaf(sc, (float)((w >> (4 * i)) & 15u), z);
-    store8(static_cast<T *>(val ? p.v : p.k) + (row0 + key) * D + c * 8, x);
+    for (int m = 0; m < 4; m++) {
+      x[2 * m] = fmaf(sc, (float)((even >> (8 * m)) & 0xffu), z);
+      x[2 * m + 1] = fmaf(sc, (float)((odd >> (8 * m)) & 0xffu), z);
+    }
+    const int j = tile * Q::KEYS + key0 + (e >> log_cpr);
+    if (j < end) store8(out + (size_t)j * D + d0 + (e & ((1 << log_cpr) - 1)) * 8, x);
   }
 }
 
@@ -291,17 +350,17 @@ template <typename T, int D, int NG>
 void append_launch(const QuantAppendParams &p, hipStream_t stream) {
   // T rows touch at most this many tiles of 32, whatever the first one's place.
   const int tiles = (p.T - 1 + kQuantTile - 1) / kQuantTile + 1;
-  const int units = p.S * p.L * p.Hkv;
-  hipLaunchKernelGGL((quant_append_kernel<T, D, NG>), dim3((uint32_t)units * (uint32_t)tiles),
-                     dim3(kAppendWaves<D> * kWave), 0, stream, p, tiles);
+  const uint32_t units = (uint32_t)p.S * p.L * p.Hkv;
+  hipLaunchKernelGGL((quant_append_kernel<T, D, NG>), dim3(units * tiles), dim3(kTileWaves<D> * kWave), 0, stream, p,
+                     tiles);
 }
 
 template <typename T, int D, int NG>
 void read_launch(const QuantReadParams &p, hipStream_t stream) {
-  const int tiles = (p.cap < p.cap_dst ? p.cap : p.cap_dst) / kQuantTile + 1;
-  const int units = p.S * p.L * p.Hkv;
-  hipLaunchKernelGGL((quant_read_kernel<T, D, NG>), dim3((uint32_t)units * (uint32_t)tiles), dim3(kThreads), 0, stream,
-                     p, tiles);
+  const int tiles = ((p.cap < p.cap_dst ? p.cap : p.cap_dst) - 1) / kQuantTile + 1;
+  const uint32_t units = (uint32_t)p.S * p.L * p.Hkv;
+  hipLaunchKernelGGL((quant_read_kernel<T, D, NG>), dim3(units * tiles), dim3(kTileWaves<D> * kWave), 0, stream, p,
+                     tiles);
 }
 
 }  // namespace
