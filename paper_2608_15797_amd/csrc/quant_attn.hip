@@ -261,7 +261,7 @@ constexpr int kRecFloats = 4 + D / 2;
 // so that p s fits float16 (s <= 2184.6), and is rarely far below 1, where
 // float16 gets coarse. The first tile of a piece sets it: a row that sees no
 // key there sees none later.
-constexpr float kSlack = 4.0f, kHead = 3.0f;
+constexpr float kSlack = 4.0f, kHead = 1.0f;
 
 __device__ __forceinline__ int ctx_tiles(const QuantAttnParams &p, int c) {
   return c < p.P ? (ctx_len(p, c) + kQuantTile - 1) / kQuantTile : 0;
@@ -350,6 +350,14 @@ __device__ __forceinline__ void load_tile(char *slot, const char *tile, bool liv
 #endif  // the host pass has no buffer-to-LDS loads
 }
 
+// With three row blocks and more the keys' values themselves are expanded, z +
+// s n as float16 (off by 2^-12 of an element at most): 15 packed instructions
+// per eight elements against five for the codes, but per key and row one fma
+// after the product instead of two and one per group. 16 contexts shared by 8
+// candidates of 6 heads 348 -> 321 us, 35 rows 328 -> 297.
+template <int RB>
+constexpr bool kKeyValues = RB >= 3;
+
 // The query operands of one row block and what is summed for it.
 template <int D, int NG>
 struct Block {
@@ -368,7 +376,22 @@ __device__ __forceinline__ u32x4 expand(uint32_t w) {
   return (u32x4){w & 0x000f000fu, w & 0x00f000f0u, h & 0x000f000fu, h & 0x00f000f0u};
 }
 
-template <int D, int NG>
+// z + s n of a code word's elements, in the order of expand(): n from 1024 + n
+// (the mantissa of a float16), exactly.
+__device__ __forceinline__ u32x4 expand_values(uint32_t w, f16_t s, f16_t z) {
+  const half2_t s2 = {s, s}, z2 = {z, z}, base = {(f16_t)1024.f, (f16_t)1024.f};
+  uint32_t bias = 0x64006400u;
+  asm("" : "+v"(bias));  // in a vector register: one and-or instruction per pair
+  u32x4 out;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const half2_t n = __builtin_bit_cast(half2_t, ((w >> (4 * i)) & 0x000f000fu) | bias) - base;
+    out[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(n, s2, z2));
+  }
+  return out;
+}
+
+template <int D, int NG, bool VALUES>
 __device__ __forceinline__ void load_queries(Block<D, NG> &b, const QuantAttnParams &p, const bf16_t *row, int lane) {
   const int g = lane >> 4;
   float x[D / 32][8];
@@ -400,9 +423,10 @@ __device__ __forceinline__ void load_queries(Block<D, NG> &b, const QuantAttnPar
       sum[i * NG / (D / 32)] += x[i][k];
     }
     b.q[i][0] = pack_f16(x[i][0], x[i][4]);
-    b.q[i][1] = pack_f16(x[i][1] * 0.0625f, x[i][5] * 0.0625f);
+    constexpr float kHigh = VALUES ? 1.f : 0.0625f;  // of codes placed four bits up
+    b.q[i][1] = pack_f16(x[i][1] * kHigh, x[i][5] * kHigh);
     b.q[i][2] = pack_f16(x[i][2], x[i][6]);
-    b.q[i][3] = pack_f16(x[i][3] * 0.0625f, x[i][7] * 0.0625f);
+    b.q[i][3] = pack_f16(x[i][3] * kHigh, x[i][7] * kHigh);
   }
   float mine = 0.f;  // the sum of group g
 #pragma unroll
@@ -442,43 +466,64 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
                                           bool first, const int *limits, int lane) {
   using Q = QTile<D, NG>;
   const int n = lane & 15, g = lane >> 4;
-  float d[RB][2][4];  // logits less the rows' references (log2)
+  float4_t d[RB][2];  // logits less the rows' references (log2)
 #pragma unroll
   for (int t = 0; t < 2; t++) {
     constexpr int PER = D / 32 / NG;  // products per group
     const u32x4 code = *reinterpret_cast<const u32x4 *>(slot + (D == 128 ? t * 1024 : 0) + lane * 16);
-    uint32_t z = *reinterpret_cast<const uint16_t *>(slot + Q::KZ + t * 32 * NG + (n * NG + (NG == 4 ? g : g & (NG - 1))) * 2);
-    if (NG < 4) z = g < NG ? z : 0u;
-    const u32x2 kz = {z | (z << 16), z};
-    uint32_t ks[2 * NG];  // scales of keys 4 g .. 4 g + 3: [key][group] float16
+    if constexpr (kKeyValues<RB>) {
+      const f16_t *sk = reinterpret_cast<const f16_t *>(slot + Q::KS) + (16 * t + n) * NG;
+      const f16_t *zk = reinterpret_cast<const f16_t *>(slot + Q::KZ) + (16 * t + n) * NG;
+      u32x4 ka[D / 32];
 #pragma unroll
-    for (int i = 0; i < 2 * NG; i++) ks[i] = *reinterpret_cast<const uint32_t *>(slot + Q::KS + t * 32 * NG + g * 8 * NG + i * 4);
-    u32x4 ka[D / 32];
+      for (int i = 0; i < D / 32; i++) ka[i] = expand_values(code[D == 128 ? i : 2 * t + i], sk[i / PER], zk[i / PER]);
 #pragma unroll
-    for (int i = 0; i < D / 32; i++) ka[i] = expand(code[D == 128 ? i : 2 * t + i]);
+      for (int i = 0; i < D / 32; i++)  // the blocks' products between the steps of one
 #pragma unroll
-    for (int b = 0; b < RB; b++) {
-      const Block<D, NG> &B = blk[b];
-      const float4_t zt = mfma_f16_k16(kz, B.qz, (float4_t){0.f, 0.f, 0.f, 0.f});
-      float xs[4];
+        for (int b = 0; b < RB; b++)
+          d[b][t] = mfma_f16(ka[i], blk[b].q[i], i == 0 ? (float4_t){0.f, 0.f, 0.f, 0.f} : d[b][t]);
+    } else {
+      uint32_t z = *reinterpret_cast<const uint16_t *>(slot + Q::KZ + t * 32 * NG + (n * NG + (NG == 4 ? g : g & (NG - 1))) * 2);
+      if (NG < 4) z = g < NG ? z : 0u;
+      const u32x2 kz = {z | (z << 16), z};
+      uint32_t ks[2 * NG];  // scales of keys 4 g .. 4 g + 3: [key][group] float16
 #pragma unroll
-      for (int k = 0; k < NG; k++) {
-        float4_t a = {0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < 2 * NG; i++) ks[i] = *reinterpret_cast<const uint32_t *>(slot + Q::KS + t * 32 * NG + g * 8 * NG + i * 4);
+      u32x4 ka[D / 32];
 #pragma unroll
-        for (int i = 0; i < PER; i++) a = mfma_f16(ka[k * PER + i], B.q[k * PER + i], a);
+      for (int i = 0; i < D / 32; i++) ka[i] = expand(code[D == 128 ? i : 2 * t + i]);
+#pragma unroll
+      for (int b = 0; b < RB; b++) {
+        const Block<D, NG> &B = blk[b];
+        const float4_t zt = mfma_f16_k16(kz, B.qz, (float4_t){0.f, 0.f, 0.f, 0.f});
+        float xs[4];
+#pragma unroll
+        for (int k = 0; k < NG; k++) {
+          float4_t a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < PER; i++) a = mfma_f16(ka[k * PER + i], B.q[k * PER + i], a);
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            const int at = j * NG + k;
+            const half2_t h = __builtin_bit_cast(half2_t, ks[at >> 1]);
+            const float sc = (float)h[at & 1];
+            xs[j] = k == 0 ? a[j] * sc : fmaf(a[j], sc, xs[j]);
+          }
+        }
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-          const int at = j * NG + k;
-          const half2_t h = __builtin_bit_cast(half2_t, ks[at >> 1]);
-          const float sc = (float)h[at & 1];
-          xs[j] = k == 0 ? a[j] * sc : fmaf(a[j], sc, xs[j]);
+          d[b][t][j] = fmaf(fmaf(xs[j], 0x1p24f, zt[j]), B.unit, B.nref);
         }
       }
-#pragma unroll
-      for (int j = 0; j < 4; j++) {
-        d[b][t][j] = fmaf(fmaf(xs[j], 0x1p24f, zt[j]), B.unit, B.nref);
-      }
     }
+  }
+  if constexpr (kKeyValues<RB>) {
+#pragma unroll
+    for (int b = 0; b < RB; b++)
+#pragma unroll
+      for (int t = 0; t < 2; t++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) d[b][t][j] = fmaf(d[b][t][j], blk[b].unit, blk[b].nref);
   }
   phase();
   u32x4 vz = *reinterpret_cast<const u32x4 *>(slot + Q::VZ + (n & (NG - 1)) * 64 + g * 16);
@@ -639,7 +684,7 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves
         row = static_cast<const bf16_t *>(p.q) + ((((size_t)s * p.L + l) * p.Hkv + h) * per + rr) * D;
         if (p.nq > 1) limit = (int)min((long)n_ctx, (long)n_ctx + own_len(p, s) - (p.nq - 1 - rr % p.nq));
       }
-      load_queries<D, NG>(blk[i], p, row, lane);
+      load_queries<D, NG, kKeyValues<RB>>(blk[i], p, row, lane);
       clear<D, NG>(blk[i]);
       if (RB <= 2) blk[i].limit = limit;
       else limits[16 * i + n] = limit;
