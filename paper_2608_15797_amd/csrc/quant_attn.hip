@@ -278,22 +278,27 @@ struct Cut {
   int first, sum;   // lane: tiles of context `lane`; of contexts 0 .. lane
 };
 
-__device__ __forceinline__ int scan_lanes(int t, int lane) {
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int o = __shfl_up(t, off, kWave);
-    if (lane >= off) t += o;
-  }
+// Inclusive sum over the lanes: within rows of 16 (by 1, 2, 4, 8), then the
+// last lanes of rows 0 and 2 into 1 and 3, then that of row 1 into 2 and 3.
+__device__ __forceinline__ int scan_lanes(int t) {
+  t += __builtin_amdgcn_update_dpp(0, t, 0x111, 0xf, 0xf, true);
+  t += __builtin_amdgcn_update_dpp(0, t, 0x112, 0xf, 0xf, true);
+  t += __builtin_amdgcn_update_dpp(0, t, 0x114, 0xf, 0xf, true);
+  t += __builtin_amdgcn_update_dpp(0, t, 0x118, 0xf, 0xf, true);
+  t += __builtin_amdgcn_update_dpp(0, t, 0x142, 0xa, 0xf, false);
+  t += __builtin_amdgcn_update_dpp(0, t, 0x143, 0xc, 0xf, false);
   return t;
 }
+// Lane i's value as a scalar.
+__device__ __forceinline__ int lane_value(int x, int i) { return __builtin_amdgcn_readlane(x, i); }
 
 __device__ __forceinline__ Cut cut_of(const QuantAttnParams &p, int lane) {
   Cut cut;
   cut.first = ctx_tiles(p, lane);
-  cut.sum = scan_lanes(cut.first, lane);
-  int sum = uniform(__shfl(cut.sum, kWave - 1, kWave));
+  cut.sum = scan_lanes(cut.first);
+  int sum = lane_value(cut.sum, kWave - 1);
   for (int c0 = kWave; c0 < p.P; c0 += kWave)
-    sum += uniform(__shfl(scan_lanes(ctx_tiles(p, c0 + lane), lane), kWave - 1, kWave));
+    sum += lane_value(scan_lanes(ctx_tiles(p, c0 + lane)), kWave - 1);
   cut.total = sum * p.L * p.Hkv;
   cut.span = max((int)(((uint32_t)cut.total + p.nwaves - 1) / (uint32_t)p.nwaves), p.min_span);
   return cut;
@@ -307,11 +312,11 @@ __device__ __forceinline__ void store_cut(const QuantAttnParams &p, const Cut &c
   int t = cut.first, sc = cut.sum, at = 0;
   for (int c0 = 0;;) {
     if (c0 + lane < p.P) to[1 + c0 + lane] = at + sc - t;
-    at += uniform(__shfl(sc, kWave - 1, kWave));
+    at += lane_value(sc, kWave - 1);
     c0 += kWave;
     if (c0 >= p.P) break;
     t = ctx_tiles(p, c0 + lane);
-    sc = scan_lanes(t, lane);
+    sc = scan_lanes(t);
   }
 }
 
@@ -449,10 +454,22 @@ __device__ __forceinline__ void clear(Block<D, NG> &b) {
   b.z = (float4_t){0.f, 0.f, 0.f, 0.f};
 }
 
-// Halfword mask of the lane's slots 2 r and 2 r + 1: all ones where the key is live.
-__device__ __forceinline__ uint32_t live_slots(int key0, int r, int g, int n_ctx) {
-  const int k0 = key0 + (r < 2 ? 4 * g + 2 * r : 16 + 4 * g + 2 * (r - 2));
-  return (k0 < n_ctx ? 0xffffu : 0u) | (k0 + 1 < n_ctx ? 0xffff0000u : 0u);
+// The key in a tile of slot 8 g + e of the values' order.
+__device__ __forceinline__ int slot_key(int g, int e) { return e < 4 ? 4 * g + e : 16 + 4 * g + e - 4; }
+
+// The last tile of a context: slots past the last hold anything, so their value
+// scales and offsets become 0 in LDS (p = 0 times a NaN would reach every row).
+template <int D, int NG>
+__device__ __forceinline__ void clear_dead_slots(char *slot, int live, int lane) {
+  using Q = QTile<D, NG>;
+#pragma unroll
+  for (int e = lane; e < 32 * NG; e += kWave) {
+    const int i = e & 7, g = (e >> 3) & 3;  // slot 8 g + i of a group
+    if (slot_key(g, i) >= live) {
+      *reinterpret_cast<uint16_t *>(slot + Q::VS + 2 * e) = 0;
+      *reinterpret_cast<uint16_t *>(slot + Q::VZ + 2 * e) = 0;
+    }
+  }
 }
 
 // Between the phases of a tile: what a phase loads from LDS is not held in
@@ -460,9 +477,9 @@ __device__ __forceinline__ uint32_t live_slots(int key0, int r, int g, int n_ctx
 __device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
 
 // One tile for RB row blocks; key0: the tile's first key; tail: some row does
-// not see some of its keys, or it has slots past the context's last.
+// not see some of its keys.
 template <int D, int NG, int RB>
-__device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *slot, int key0, int n_ctx, bool tail,
+__device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *slot, int key0, bool tail,
                                           bool first, const int *limits, int lane) {
   using Q = QTile<D, NG>;
   const int n = lane & 15, g = lane >> 4;
@@ -536,9 +553,6 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
 #pragma unroll
         for (int j = 0; j < 4; j++)
           d[b][t][j] = key0 + 16 * t + 4 * g + j < (RB <= 2 ? blk[b].limit : limits[16 * b + n]) ? d[b][t][j] : kNegInf;
-    // Slots past the last hold anything: their scales and offsets become 0.
-#pragma unroll
-    for (int r = 0; r < 4; r++) vz[r] &= live_slots(key0, r, g, n_ctx);
   }
   // Column NG holds ones; what the columns after it hold is not used.
 #pragma unroll
@@ -586,15 +600,6 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
     u32x4 vs[GH];
 #pragma unroll
     for (int i = 0; i < GH; i++) vs[i] = *reinterpret_cast<const u32x4 *>(slot + Q::VS + (h * GH + i) * 64 + g * 16);
-    if (tail) {
-      asm volatile("");
-#pragma unroll
-      for (int r = 0; r < 4; r++) {
-        const uint32_t m = live_slots(key0, r, g, n_ctx);
-#pragma unroll
-        for (int i = 0; i < GH; i++) vs[i][r] &= m;
-      }
-    }
     const u32x4 code = *reinterpret_cast<const u32x4 *>(slot + Q::VC + h * 1024 + lane * 16);
     u32x4 vb[4];
 #pragma unroll
@@ -653,13 +658,13 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves
     if (past) {
       const int i = uniform(__ffsll((long long)past) - 1);
       c += i;
-      at += uniform(__shfl(sc - t, i, kWave));
+      at += lane_value(sc - t, i);
       break;
     }
-    at += uniform(__shfl(sc, kWave - 1, kWave));
+    at += lane_value(sc, kWave - 1);
     c += kWave;
     t = ctx_tiles(p, c + lane);
-    sc = scan_lanes(t, lane);
+    sc = scan_lanes(t);
   }
   int n_ctx = uniform(ctx_len(p, c)), tiles = (n_ctx + kQuantTile - 1) / kQuantTile;
   int u = (pos - at * lh) / tiles;  // unit within the context
@@ -703,7 +708,8 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves
       wait_lds();  // the slot's tile has been read
       load_tile<D, NG>(ring + next * SLOT, base + (size_t)tn * Q::BYTES, tn < last, lane);
       wait_vm<LOADS *(DEPTH - 1)>();
-      tile_step<D, NG, RB>(blk, ring + at_slot * SLOT, t * Q::KEYS, n_ctx, (t + 1) * Q::KEYS > least, t == tile, limits, lane);
+      if ((t + 1) * Q::KEYS > n_ctx) clear_dead_slots<D, NG>(ring + at_slot * SLOT, n_ctx - t * Q::KEYS, lane);
+      tile_step<D, NG, RB>(blk, ring + at_slot * SLOT, t * Q::KEYS, (t + 1) * Q::KEYS > least, t == tile, limits, lane);
       at_slot = at_slot + 1 == DEPTH ? 0 : at_slot + 1;
     }
     wait_vm<0>();  // the zeros behind the last tile, before the ring starts again
@@ -754,8 +760,6 @@ struct OwnChunk {
   u32x4 k[2][D / 32];
   uint32_t v[8][D / 32];
 };
-
-__device__ __forceinline__ int slot_key(int g, int e) { return e < 4 ? 4 * g + e : 16 + 4 * g + e - 4; }
 
 // The own rows of a unit and the query rows r0 .. r0 + nrow - 1 of its
 // sequence. Rows before `first` are in the cache, the new ones after it in the
@@ -831,15 +835,25 @@ __device__ __forceinline__ void load_values(OwnChunk<D> &c, const OwnUnit &w, in
   }
 }
 
-// The records of a unit (context c, unit u of it) by waves w0 .. w1 of the context kernel.
+// Where the records of context c's units are: what is loaded of it, and the
+// waves w0 .. w1 of the context kernel that left records of unit u.
+struct RecordPlan {
+  int span, before, len;
+  __device__ __forceinline__ RecordPlan(const QuantAttnParams &p, int c) {
+    const int *cut = reinterpret_cast<const int *>(p.ws);
+    span = cut[0];
+    before = cut[1 + c];
+    len = p.ctx_len[c];
+  }
+};
 struct Records {
   int w0, w1;
 };
-__device__ __forceinline__ Records records_of(const QuantAttnParams &p, int c, int u) {
-  const int *cut = reinterpret_cast<const int *>(p.ws);
-  const int span = uniform(cut[0]), before = uniform(cut[1 + c]), tiles = uniform(ctx_tiles(p, c));
-  const int first = before * p.L * p.Hkv + u * tiles;
-  return Records{first / span, tiles > 0 ? (first + tiles - 1) / span : first / span - 1};
+__device__ __forceinline__ Records records_of(const QuantAttnParams &p, const RecordPlan &plan, int u) {
+  const int tiles = (min(max(uniform(plan.len), 0), p.cap) + kQuantTile - 1) / kQuantTile;
+  const uint32_t span = uniform(plan.span), first = uniform(plan.before) * p.L * p.Hkv + u * tiles;
+  const int w0 = first / span;
+  return Records{w0, tiles > 0 ? (int)((first + tiles - 1) / span) : w0 - 1};
 }
 
 // What a wave has of the own rows: 16 query rows (lane's row: n), running
@@ -1016,6 +1030,7 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(2))) void
   const int unit = blockIdx.x / blocks, r0 = blockIdx.x % blocks * 16;
   const int lh = p.L * p.Hkv, s = unit / lh, c = s / p.C;
   const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
+  const RecordPlan plan(p, c);
   const int u = uniform(own_len(p, s)), nrow = min(16, per - r0);
   OwnState<D> st;
   st.m = kNegInf;
@@ -1029,7 +1044,7 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(2))) void
     load_values<D>(ch, w, 0, lane);
     own_begin<D>(st, p, w, unit, lane);
   }
-  const Records here = records_of(p, c, unit % lh);
+  const Records here = records_of(p, plan, unit % lh);
   own_attend<D>(st, ch, w, 0, 32, lane);
   if (p.ok && r0 == 0) store_new<bf16_t, D, kWave>(p, unit, s, u);
   st.den += shfl_xor(st.den, 16);
@@ -1063,21 +1078,21 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(2))) void
 constexpr int kOwnWaves = 4;
 
 // Second kernel, few units: a workgroup per (sequence, layer, KV head) and rpw
-// of its rows. Its waves attend to the own rows, 32 keys each in turn; then
+// of its rows. Its four waves attend to the own rows, 32 keys each in turn; then
 // all of them join these and the context's records: 16 lanes per row, the
-// records of a row dealt to 16 / rpw groups.
+// records of a row dealt to the groups of 16.
 template <int D, int NG>
 __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_eu(2))) void quant_join(QuantAttnParams p) {
-  constexpr int NT = kOwnWaves * kWave, EL = D / 16;  // elements per thread of the join
+  constexpr int NT = kOwnWaves * kWave, SLOTS = NT / 16, EL = D / 16;  // elements per thread of the join
   __shared__ float so[kOwnWaves][16][D];
-  __shared__ float sm[16][2];
+  __shared__ float sm[SLOTS][2];
   __shared__ float wm[kOwnWaves][16], wl[kOwnWaves][16];
   const int per = p.nq * p.G, blocks = (per + p.rpw - 1) / p.rpw;
   const int unit = blockIdx.x / blocks, r0 = blockIdx.x % blocks * p.rpw;
   const int lh = p.L * p.Hkv, s = unit / lh, c = s / p.C;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, n = lane & 15, g = lane >> 4;
-  const int u = uniform(own_len(p, s));
-  const int nrow = min(p.rpw, per - r0);
+  const RecordPlan plan(p, c);
+  const int u = uniform(own_len(p, s)), nrow = min(p.rpw, per - r0);
 
   const OwnUnit w = own_unit<D>(p, unit, u, r0, nrow);
   OwnState<D> st;
@@ -1087,7 +1102,7 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
     load_values<D>(ch, w, wave * 32, lane);
     own_begin<D>(st, p, w, unit, lane);
   }
-  const Records here = records_of(p, c, unit % lh);
+  const Records here = records_of(p, plan, unit % lh);
   if (p.ok && r0 == 0) store_new<bf16_t, D, NT>(p, unit, s, u);
 
   if (u > 0) {
@@ -1107,52 +1122,55 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
   }
   __syncthreads();
 
-  // Join. Thread: row r0 + slot % rpw, records part, part + parts, .. of it, elements sub EL ..
-  const int slot = tid / 16, sub = tid % 16, parts = 16 / p.rpw;
+  // Join. Thread: row r0 + slot % rpw, records part, part + parts, .. of it,
+  // elements sub EL ..
+  const int slot = tid / 16, sub = tid % 16, parts = SLOTS / p.rpw;
   const int row = slot % p.rpw, part = slot / p.rpw;
   float m = kNegInf, den = 0.f, o[EL];
 #pragma unroll
   for (int e = 0; e < EL; e++) o[e] = 0.f;
-  if (row < nrow) {
-    if (part == 0 && u > 0) {
+  if (row < nrow && part == 0 && u > 0) {
 #pragma unroll
-      for (int w = 0; w < kOwnWaves; w++) {
-        float x[EL];
+    for (int w = 0; w < kOwnWaves; w++) {
+      float x[EL];
 #pragma unroll
-        for (int e = 0; e < EL; e++) x[e] = so[w][row][sub * EL + e];
-        fold<EL>(m, den, o, wm[w][row], wl[w][row], 1.f, x);
-      }
+      for (int e = 0; e < EL; e++) x[e] = so[w][row][sub * EL + e];
+      fold<EL>(m, den, o, wm[w][row], wl[w][row], 1.f, x);
     }
-    {
-      const int rows = p.C * per, r = s % p.C * per + r0 + row;
-      const float *rec = records(p) + (((size_t)(here.w0 + part) + (size_t)c * lh + unit % lh) * rows + r) * kRecFloats<D>;
+  }
+  if (row < nrow) {
+    const int rows = p.C * per, r = s % p.C * per + r0 + row;
+    const float *rec = records(p) + (((size_t)(here.w0 + part) + (size_t)c * lh + unit % lh) * rows + r) * kRecFloats<D>;
 #pragma unroll 4
-      for (int k = here.w0 + part; k <= here.w1; k += parts, rec += (size_t)parts * rows * kRecFloats<D>) {
-        const float2_t ml = *reinterpret_cast<const float2_t *>(rec);
-        float x[EL];
-        record_values<EL>(rec, sub, x);
-        fold<EL>(m, den, o, ml[0], ml[1], ml[1], x);
-      }
+    for (int k = here.w0 + part; k <= here.w1; k += parts, rec += (size_t)parts * rows * kRecFloats<D>) {
+      const float2_t ml = *reinterpret_cast<const float2_t *>(rec);
+      float x[EL];
+      record_values<EL>(rec, sub, x);
+      fold<EL>(m, den, o, ml[0], ml[1], ml[1], x);
     }
   }
   if (parts > 1) {
-    __syncthreads();
+    // Halves of the groups join the others, down to one per row.
     float *po = &so[0][0][0];
+    for (int half = parts / 2;; half /= 2) {
+      __syncthreads();
+      if (part < 2 * half) {
 #pragma unroll
-    for (int e = 0; e < EL; e++) po[slot * D + sub * EL + e] = o[e];
-    if (sub == 0) {
-      sm[slot][0] = m;
-      sm[slot][1] = den;
-    }
-    __syncthreads();
-    if (part == 0) {
-      for (int k = 1; k < parts; k++) {
+        for (int e = 0; e < EL; e++) po[slot * D + sub * EL + e] = o[e];
+        if (sub == 0) {
+          sm[slot][0] = m;
+          sm[slot][1] = den;
+        }
+      }
+      __syncthreads();
+      if (part < half) {
         float x[EL];
-        const int from = k * p.rpw + row;
+        const int from = slot + half * p.rpw;
 #pragma unroll
         for (int e = 0; e < EL; e++) x[e] = po[from * D + sub * EL + e];
         fold<EL>(m, den, o, sm[from][0], sm[from][1], 1.f, x);
       }
+      if (half == 1) break;
     }
   }
   if (part == 0 && row < nrow)
@@ -1160,7 +1178,7 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
 }
 
 constexpr int kChipSimds = 1024;  // 256 CUs of four
-constexpr int kMinSpan = 4;
+constexpr int kMinSpan = 2;
 constexpr int kMaxBlocks = 4;     // row blocks a wave takes at once
 
 // Plan of a bfloat16 call, from shapes alone.
