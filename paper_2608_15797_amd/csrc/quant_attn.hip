@@ -625,19 +625,18 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
 }
 
 // Waves per SIMD and tiles in a wave's ring. One wave's registers hold up to
-// three row blocks beside another's; two waves' rings of four 5 KiB tiles each
+// three row blocks beside another's at D = 128, a fourth of one at D = 64 (18.2
+// us against 18.7 with two waves for 61 contexts of up to 2000); two waves' rings of four 5 KiB tiles each
 // are all of a CU's LDS. 32 contexts of 16384 in groups of 64: rings of two,
 // three and four tiles 620, 656 and 588 us, three waves with two tiles 590.
-template <int RB>
-constexpr int kCtxWaves = RB <= 3 ? 2 : 1;
-template <int RB>
-constexpr int kCtxDepth = RB <= 2 ? 4 : RB == 3 ? 3 : 6;
+constexpr int ctx_waves(int D, int RB) { return RB > 3 ? 1 : D == 128 || RB == 3 ? 2 : RB == 2 ? 3 : 4; }
+constexpr int ctx_depth(int RB) { return RB <= 2 ? 4 : RB == 3 ? 3 : 6; }
 
 // Context kernel: one wave per span.
 template <int D, int NG, int RB>
-__global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(kCtxWaves<RB>))) void quant_ctx(QuantAttnParams p) {
+__global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(ctx_waves(D, RB)))) void quant_ctx(QuantAttnParams p) {
   using Q = QTile<D, NG>;
-  constexpr int DEPTH = kCtxDepth<RB>, LOADS = Ring<D, NG>::LOADS, SLOT = Ring<D, NG>::SLOT;
+  constexpr int DEPTH = ctx_depth(RB), LOADS = Ring<D, NG>::LOADS, SLOT = Ring<D, NG>::SLOT;
   __shared__ __align__(1024) char ring[DEPTH * SLOT];
   __shared__ int limits[RB <= 2 ? 1 : RB * 16];  // visible keys of each row, beyond two blocks (registers)
   const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
@@ -787,7 +786,9 @@ __device__ __forceinline__ rsrc_t held_rows(const bf16_t *rows, const OwnUnit &w
   return make_rsrc(rows + (size_t)key0 * D, (uint32_t)max(w.first - key0, 0) * (2 * D));
 }
 
-template <int D>
+// ONE: a single query token, so at most one new row, the last: its lanes' words
+// are loaded beside (registers: 20 words instead of a second chunk).
+template <int D, bool ONE>
 __device__ __forceinline__ void load_keys(OwnChunk<D> &c, const OwnUnit &w, int key0, int lane) {
   constexpr int ROW = 2 * D;
   const int n = lane & 15, g = lane >> 4;
@@ -797,9 +798,22 @@ __device__ __forceinline__ void load_keys(OwnChunk<D> &c, const OwnUnit &w, int 
 #pragma unroll
     for (int i = 0; i < D / 32; i++)
       c.k[t][i] = __builtin_amdgcn_raw_buffer_load_b128(held, n * ROW + g * 16 + t * 16 * ROW + i * 64, 0, kStreamLoad);
-  if (key0 + 32 > w.first && w.first < w.u) {
-    // New rows; those before the first get an offset past the end.
-    const rsrc_t fresh = make_rsrc(w.fk, w.nq * ROW);
+  if (key0 + 32 <= w.first || w.first == w.u) return;
+  const rsrc_t fresh = make_rsrc(w.fk, w.nq * ROW);
+  if constexpr (ONE) {
+    const int key = w.first - key0;
+    const uint32_t off = n == (key & 15) ? g * 16 : 0x40000000u;
+    u32x4 x[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; i++) x[i] = __builtin_amdgcn_raw_buffer_load_b128(fresh, off + i * 64, 0, kStreamLoad);
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+      if (t == key >> 4) {
+#pragma unroll
+        for (int i = 0; i < D / 32; i++) c.k[t][i] |= x[i];
+      }
+  } else {
+    // Rows before the first new one get an offset past the end.
 #pragma unroll
     for (int t = 0; t < 2; t++) {
       const uint32_t off = (uint32_t)((key0 + 16 * t + n - w.first) * ROW);
@@ -810,7 +824,7 @@ __device__ __forceinline__ void load_keys(OwnChunk<D> &c, const OwnUnit &w, int 
   }
 }
 
-template <int D>
+template <int D, bool ONE>
 __device__ __forceinline__ void load_values(OwnChunk<D> &c, const OwnUnit &w, int key0, int lane) {
   constexpr int ROW = 2 * D;
   const int n = lane & 15, g = lane >> 4;
@@ -828,8 +842,19 @@ __device__ __forceinline__ void load_values(OwnChunk<D> &c, const OwnUnit &w, in
   const rsrc_t held = held_rows<D>(w.v, w, key0);
 #pragma unroll
   for (int e = 0; e < 8; e++) get(held, slot_key(g, e) * ROW, c.v[e], false);
-  if (key0 + 32 > w.first && w.first < w.u) {
-    const rsrc_t fresh = make_rsrc(w.fv, w.nq * ROW);
+  if (key0 + 32 <= w.first || w.first == w.u) return;
+  const rsrc_t fresh = make_rsrc(w.fv, w.nq * ROW);
+  if constexpr (ONE) {
+    const int key = w.first - key0, slot = 4 * (key >> 4) + (key & 3);
+    uint32_t x[D / 32];
+    get(fresh, g == ((key >> 2) & 3) ? 0u : 0x40000000u, x, false);
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+      if (e == slot) {
+#pragma unroll
+        for (int i = 0; i < D / 32; i++) c.v[e][i] |= x[i];
+      }
+  } else {
 #pragma unroll
     for (int e = 0; e < 8; e++) get(fresh, (uint32_t)((key0 + slot_key(g, e) - w.first) * ROW), c.v[e], true);
   }
@@ -890,7 +915,7 @@ __device__ __forceinline__ u32x4 value_operand(const uint32_t (&v)[8][D / 32], i
 }
 
 // One chunk at key0; `next` follows it.
-template <int D>
+template <int D, bool ONE>
 __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const OwnUnit &w, int key0, int next,
                                          int lane) {
   const int g = lane >> 4;
@@ -906,7 +931,7 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
       top = fmaxf(top, x[t][j]);
     }
   }
-  if (next < w.u) load_keys<D>(ch, w, next, lane);
+  if (next < w.u) load_keys<D, ONE>(ch, w, next, lane);
   top = fmaxf(top, shfl_xor(top, 16));
   top = fmaxf(top, shfl_xor(top, 32));
   const float mn = fmaxf(st.m, top), ref = mn == kNegInf ? 0.f : mn;
@@ -936,7 +961,7 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
   // would reach the others as 0 times it: those get a product per query token.
   const int sees_all = w.u - (w.nq - 1);
   bool split = false;
-  if (key0 + 32 > sees_all && w.nq > 1) {
+  if (!ONE && key0 + 32 > sees_all && w.nq > 1) {
     bool odd = false;
 #pragma unroll
     for (int e = 0; e < 8; e++) {
@@ -950,13 +975,13 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
     }
     split = __any(odd);
   }
-  if (!split) {
+  if (ONE || !split) {
 #pragma unroll
     for (int b = 0; b < D / 16; b++) {
       const u32x4 v = value_operand<D>(ch.v, b);
       st.o[b] = mfma_bf16(lo, v, mfma_bf16(hi, v, st.o[b]));
     }
-    if (next < w.u) load_values<D>(ch, w, next, lane);
+    if (next < w.u) load_values<D, ONE>(ch, w, next, lane);
     return;
   }
 #pragma unroll 1
@@ -978,17 +1003,17 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
       for (int j = 0; j < 4; j++) st.o[b][j] = (w.r0 + 4 * g + j) % w.nq == t ? acc[j] : st.o[b][j];
     }
   }
-  if (next < w.u) load_values<D>(ch, w, next, lane);
+  if (next < w.u) load_values<D, ONE>(ch, w, next, lane);
 }
 
 // The chunks key0, key0 + stride, .. of a unit. A chunk's keys make way for the
 // next one's once they are multiplied, its values likewise, so that those are
 // under way meanwhile. p is split into two bfloat16 terms, so that its rounding
 // (2^-17) stays out of the result.
-template <int D>
+template <int D, bool ONE>
 __device__ __forceinline__ void own_attend(OwnState<D> &st, OwnChunk<D> &ch, const OwnUnit &w, int key0, int stride,
                                            int lane) {
-  for (; key0 < w.u; key0 += stride) own_step<D>(st, ch, w, key0, key0 + stride, lane);
+  for (; key0 < w.u; key0 += stride) own_step<D, ONE>(st, ch, w, key0, key0 + stride, lane);
 }
 
 // Joins (mr, lr, values x whose sum of weights is lr after the factor scale) to a row's (m, den, o).
@@ -1023,8 +1048,8 @@ __device__ __forceinline__ void put_row(bf16_t *row, int sub, const float (&o)[E
 // Second kernel, many units: a wave per (sequence, layer, KV head) and 16 of
 // its rows attends to the own rows, 32 keys at a time, and joins the context's
 // records as it holds its result: 16 lanes per row, four rows per lane.
-template <int D, int NG>
-__global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(2))) void quant_join_wave(QuantAttnParams p) {
+template <int D, int NG, bool ONE>
+__global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(ONE ? 3 : 2))) void quant_join_wave(QuantAttnParams p) {
   constexpr int EL = D / 16;
   const int per = p.nq * p.G, blocks = (per + 15) / 16;
   const int unit = blockIdx.x / blocks, r0 = blockIdx.x % blocks * 16;
@@ -1040,12 +1065,12 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(2))) void
   const OwnUnit w = own_unit<D>(p, unit, u, r0, nrow);
   OwnChunk<D> ch;
   if (u > 0) {
-    load_keys<D>(ch, w, 0, lane);
-    load_values<D>(ch, w, 0, lane);
+    load_keys<D, ONE>(ch, w, 0, lane);
+    load_values<D, ONE>(ch, w, 0, lane);
     own_begin<D>(st, p, w, unit, lane);
   }
   const Records here = records_of(p, plan, unit % lh);
-  own_attend<D>(st, ch, w, 0, 32, lane);
+  own_attend<D, ONE>(st, ch, w, 0, 32, lane);
   if (p.ok && r0 == 0) store_new<bf16_t, D, kWave>(p, unit, s, u);
   st.den += shfl_xor(st.den, 16);
   st.den += shfl_xor(st.den, 32);
@@ -1098,15 +1123,15 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
   OwnState<D> st;
   OwnChunk<D> ch;
   if (u > 0) {
-    load_keys<D>(ch, w, wave * 32, lane);
-    load_values<D>(ch, w, wave * 32, lane);
+    load_keys<D, false>(ch, w, wave * 32, lane);
+    load_values<D, false>(ch, w, wave * 32, lane);
     own_begin<D>(st, p, w, unit, lane);
   }
   const Records here = records_of(p, plan, unit % lh);
   if (p.ok && r0 == 0) store_new<bf16_t, D, NT>(p, unit, s, u);
 
   if (u > 0) {
-    own_attend<D>(st, ch, w, wave * 32, kOwnWaves * 32, lane);
+    own_attend<D, false>(st, ch, w, wave * 32, kOwnWaves * 32, lane);
     st.den += shfl_xor(st.den, 16);
     st.den += shfl_xor(st.den, 32);
     if (g == 0) {
@@ -1187,7 +1212,7 @@ void plan(QuantAttnParams *p) {
   p->row_groups = (blocks + kMaxBlocks - 1) / kMaxBlocks;
   p->rb = (blocks + p->row_groups - 1) / p->row_groups;
   const double tiles = (double)p->P * p->L * p->Hkv * p->ntiles;
-  const int waves = kChipSimds * (p->rb <= 3 ? kCtxWaves<3> : kCtxWaves<4>);
+  const int waves = kChipSimds * ctx_waves(p->D, p->rb);
   const int most = waves / p->row_groups > 64 ? waves / p->row_groups : 64;
   p->min_span = kMinSpan;
   const double want = tiles / kMinSpan + 1;
@@ -1218,7 +1243,8 @@ void launch_bf16(const QuantAttnParams &p, hipStream_t stream) {
   }
   const int per = p.nq * p.G, rpw = p.join_waves ? 16 : p.rpw;
   const dim3 groups((uint32_t)p.S * p.L * p.Hkv * ((per + rpw - 1) / rpw));
-  if (p.join_waves) hipLaunchKernelGGL((quant_join_wave<D, NG>), groups, dim3(kWave), 0, stream, p);
+  if (p.join_waves && p.nq == 1) hipLaunchKernelGGL((quant_join_wave<D, NG, true>), groups, dim3(kWave), 0, stream, p);
+  else if (p.join_waves) hipLaunchKernelGGL((quant_join_wave<D, NG, false>), groups, dim3(kWave), 0, stream, p);
   else hipLaunchKernelGGL((quant_join<D, NG>), groups, dim3(kOwnWaves * kWave), 0, stream, p);
 }
 
