@@ -551,7 +551,8 @@ int kvr_quant_read(const kvr_quant_cache *src, const kvr_cache *dst, const int32
  *               and S a multiple of ctx->S, and [S] int32 device live lengths
  *               including the nq new tokens where k_new is given.
  *   q, out    : [S][L][Hq][nq][D] of `dtype`, Hq = G * Hkv, 1 <= G <= 16.
- *   dtype     : KVR_BF16, or KVR_F32 (a vector kernel, meant for validation).
+ *   dtype     : KVR_BF16, or KVR_F32 (a vector kernel, as elsewhere in this
+ *               library; it reads a shared context once per sequence).
  *   k_new, v_new : [S][L][Hkv][nq][D] rows of the query tokens, written to own
  *               slots len[s] - nq .. len[s] - 1 (those below 0 are not written,
  *               but attended to by nobody) and attended to in the same call; or

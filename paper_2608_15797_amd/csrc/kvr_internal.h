@@ -223,6 +223,7 @@ struct QuantAttnParams {
   // the context kernel and their least span in tiles, rows per workgroup of
   // the join, or a wave each.
   int rb, row_groups, nwaves, min_span, rpw, join_waves;
+  int shares;  // of a float32 call's keys
 };
 size_t quant_attn_workspace_bytes(const QuantAttnParams &p);
 hipError_t launch_quant_attn(const QuantAttnParams &p, hipStream_t stream);

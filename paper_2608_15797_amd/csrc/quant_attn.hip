@@ -16,20 +16,13 @@ namespace {
 
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr int kThreads = 256;
-constexpr int kMaxG = 16;
-
-__device__ __forceinline__ float as_f32(bf16_t x) { return bf16_to_f32(x); }
-__device__ __forceinline__ float as_f32(float x) { return x; }
-__device__ __forceinline__ void put(bf16_t *p, float x) { *p = (bf16_t)(pack_bf16x2(x, x) & 0xffffu); }
-__device__ __forceinline__ void put(float *p, float x) { *p = x; }
 
 // Own row j of a unit: the new rows come from the caller's arrays (another
 // workgroup may be storing them), the others from the cache.
-template <typename T>
 struct OwnRows {
-  const T *cache, *fresh;
+  const float *cache, *fresh;
   int first;  // first new row; none where fresh is NULL
-  __device__ __forceinline__ const T *row(int j, int D) const {
+  __device__ __forceinline__ const float *row(int j, int D) const {
     return fresh && j >= first ? fresh + (size_t)(j - first) * D : cache + (size_t)j * D;
   }
 };
@@ -58,140 +51,182 @@ __device__ __forceinline__ void store_new(const QuantAttnParams &p, int unit, in
       if (first + t >= 0) p.pos[(size_t)unit * p.ocap + first + t] = p.new_pos[(size_t)s * p.nq + t];
 }
 
-// Vector kernel, the float32 path: one workgroup per (sequence, layer, KV
-// head, query token). Chunks of one key per thread: the thread's key is
-// expanded and multiplied with the G query rows (in LDS), the probabilities go
-// to LDS, and each thread sums one column d over every KG-th key of the chunk.
-template <typename T, int D, int NG>
+// float32: vector kernel, one workgroup per (sequence, layer, KV head), 16 of
+// its rows and a share of its keys. 32 keys at a time are expanded to float32
+// rows in LDS; a thread has two of the 16 x 32 logits, then one column of the
+// output for some of the rows. Shares leave records (max, sum, -, -, o) that
+// quant_vector_join joins. Bound by latency in small calls, by the vector
+// units' float32 rate in long ones.
+constexpr int kVecKeys = 32, kVecRows = 16;
+
+__host__ __device__ __forceinline__ int vector_blocks(const QuantAttnParams &p) {
+  return (p.nq * p.G + kVecRows - 1) / kVecRows;
+}
+template <int D>
+constexpr int kVecRec = 4 + D;
+
+template <int D, int NG>
 __global__ __launch_bounds__(kThreads) void quant_attn_vector(QuantAttnParams p) {
   using Q = QTile<D, NG>;
-  constexpr int KG = kThreads / D, NW = kThreads / kWave;
-  __shared__ float qs[kMaxG][D];
-  __shared__ float prob[kMaxG][kThreads];
-  __shared__ float red[kMaxG][NW];
-  const int t = blockIdx.x % p.nq, unit = blockIdx.x / p.nq;
-  const int lh = p.L * p.Hkv, s = unit / lh, h = unit % p.Hkv, l = unit / p.Hkv % p.L;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, G = p.G;
-  const int c = s / p.C, n = ctx_len(p, c), u = own_len(p, s);
-  const long seen = (long)n + u - (p.nq - 1 - t);  // keys query t attends to
-  if (t == 0 && p.ok) store_new<T, D, kThreads>(p, unit, s, u);
-  const size_t qrow = (((size_t)s * p.L + l) * p.Hq + (size_t)h * G) * p.nq + t;  // + g nq
-  for (int e = tid; e < G * D; e += kThreads)
-    qs[e / D][e % D] = as_f32(static_cast<const T *>(p.q)[(qrow + (size_t)(e / D) * p.nq) * D + e % D]);
-  __syncthreads();
-
+  constexpr int CH = D / 8, PITCH = D + 4, KG = kThreads / D, RPT = kVecRows / KG;
+  __shared__ __align__(16) float qs[kVecRows][D];
+  __shared__ __align__(16) float kt[kVecKeys][PITCH], vt[kVecKeys][PITCH];
+  __shared__ float prob[kVecRows][kVecKeys + 1];
+  __shared__ float row_m[kVecRows], row_l[kVecRows], row_f[kVecRows];
+  __shared__ int row_lim[kVecRows];
+  const int blocks = vector_blocks(p), per = p.nq * p.G;
+  const int share = blockIdx.x % p.shares, ub = blockIdx.x / p.shares, block = ub % blocks, unit = ub / blocks;
+  const int lh = p.L * p.Hkv, s = unit / lh, c = s / p.C;
+  const int tid = threadIdx.x, r0 = block * kVecRows, nrow = min(kVecRows, per - r0);
+  const int n = ctx_len(p, c), u = own_len(p, s);
+  if (share == 0 && block == 0 && p.ok) store_new<float, D, kThreads>(p, unit, s, u);
+  const float *q = static_cast<const float *>(p.q) + ((size_t)unit * per + r0) * D;
+  for (int e = tid; e < kVecRows * D; e += kThreads) qs[e / D][e % D] = e < nrow * D ? q[e] : 0.f;
+  if (tid < kVecRows) {
+    row_m[tid] = kNegInf;
+    row_l[tid] = 0.f;
+    // Keys that the row sees, of context and own together.
+    row_lim[tid] = (int)((long)n + u - (p.nq - 1 - (r0 + tid) % p.nq));
+  }
   const char *ctx = static_cast<const char *>(p.data) + ((size_t)c * lh + unit % lh) * p.ntiles * Q::BYTES;
   const size_t own0 = (size_t)unit * p.ocap * D, new0 = (size_t)unit * p.nq * D;
-  const T *fk = static_cast<const T *>(p.k_new), *fv = static_cast<const T *>(p.v_new);
-  const OwnRows<T> K{static_cast<const T *>(p.ok) + own0, fk ? fk + new0 : nullptr, u - p.nq};
-  const OwnRows<T> V{static_cast<const T *>(p.ov) + own0, fv ? fv + new0 : nullptr, u - p.nq};
-  float m[kMaxG], den[kMaxG], o[kMaxG];
+  const float *fk = static_cast<const float *>(p.k_new), *fv = static_cast<const float *>(p.v_new);
+  const OwnRows K{static_cast<const float *>(p.ok) + own0, fk ? fk + new0 : nullptr, u - p.nq};
+  const OwnRows V{static_cast<const float *>(p.ov) + own0, fv ? fv + new0 : nullptr, u - p.nq};
+  const int d = tid % D, kg = tid / D, key = tid % kVecKeys, rg = tid / kVecKeys;
+  const int sees_all = (int)((long)n + u - (p.nq - 1));  // keys before it are seen by every row
+  float o[RPT];
 #pragma unroll
-  for (int g = 0; g < kMaxG; g++) {
-    m[g] = kNegInf;
-    den[g] = o[g] = 0.f;
-  }
-  const int d = tid % D, kg = tid / D;
-  for (long c0 = 0; c0 < seen; c0 += kThreads) {
-    const long key = c0 + tid;
-    float x[kMaxG];
+  for (int i = 0; i < RPT; i++) o[i] = 0.f;
+
+  // Chunks: the context's tiles, then the own rows in 32s.
+  const int held = (n + kVecKeys - 1) / kVecKeys, all = held + (u + kVecKeys - 1) / kVecKeys;
+  const int t0 = (int)((long)all * share / p.shares), t1 = (int)((long)all * (share + 1) / p.shares);
+  for (int t = t0; t < t1; t++) {
+    const bool own = t >= held;
+    const int first = own ? n + (t - held) * kVecKeys : t * kVecKeys;  // token of the chunk's first key
+    const int live = min(kVecKeys, own ? n + u - first : n - first);
+    const char *tile = ctx + (size_t)t * Q::BYTES;
+    __syncthreads();
+    for (int e = tid; e < 2 * kVecKeys * CH; e += kThreads) {
+      const bool val = e >= kVecKeys * CH;
+      const int k = e / CH % kVecKeys, ch = e % CH;
+      float x[8];
+      if (k >= live) {
 #pragma unroll
-    for (int g = 0; g < kMaxG; g++) x[g] = 0.f;
-    if (key < seen) {
-      const bool held = key < n;
-      const char *tile = ctx + (held ? key / Q::KEYS : 0) * Q::BYTES;
-      const int kt = (int)(key % Q::KEYS);
-      const T *krow = held ? nullptr : K.row((int)(key - n), D);
-      for (int ch = 0; ch < D / 8; ch++) {
-        float k8[8];
-        if (held) {
-          const uint32_t w = *reinterpret_cast<const uint32_t *>(tile + Q::kword(kt, ch));
-          const int at = Q::kparam(kt, ch * 8 / Q::GROUP);
-          const float sc = f16_at(tile + Q::KS + at), z = f16_at(tile + Q::KZ + at);
+        for (int i = 0; i < 8; i++) x[i] = 0.f;
+      } else if (own) {
+        const float *row = (val ? V : K).row(first - n + k, D) + ch * 8;
 #pragma unroll
-          for (int i = 0; i < 8; i++) k8[i] = fmaf(sc, (float)((w >> (4 * i)) & 15u), z);
+        for (int h = 0; h < 2; h++) {
+          const float4_t w = reinterpret_cast<const float4_t *>(row)[h];
+#pragma unroll
+          for (int i = 0; i < 4; i++) x[4 * h + i] = w[i];
+        }
+      } else {
+        const int grp = ch * 8 / Q::GROUP, at = val ? Q::VS + Q::vparam(k, grp) : Q::KS + Q::kparam(k, grp);
+        const float sc = f16_at(tile + at), z = f16_at(tile + at + (Q::KZ - Q::KS));
+        uint32_t w = 0;
+        if (!val) {
+          w = *reinterpret_cast<const uint32_t *>(tile + Q::kword(k, ch));
         } else {
 #pragma unroll
-          for (int i = 0; i < 8; i++) k8[i] = as_f32(krow[ch * 8 + i]);
+          for (int i = 0; i < 4; i++) w |= (uint32_t)(uint8_t)tile[Q::vbyte(k, ch * 4 + i)] << (8 * i);
         }
 #pragma unroll
-        for (int g = 0; g < kMaxG; g++)
-          if (g < G) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) x[g] = fmaf(qs[g][ch * 8 + i], k8[i], x[g]);
-          }
+        for (int i = 0; i < 8; i++) x[i] = fmaf(sc, (float)((w >> (4 * i)) & 15u), z);
       }
-    }
-#pragma unroll
-    for (int g = 0; g < kMaxG; g++)
-      if (g < G) {
-        x[g] = key < seen ? x[g] * p.scale * kLog2e : kNegInf;
-        const float wm = wave_max(x[g]);
-        if (lane == 0) red[g][wave] = wm;
-      }
-    __syncthreads();
-    float keep[kMaxG];
-#pragma unroll
-    for (int g = 0; g < kMaxG; g++)
-      if (g < G) {
-        float mn = m[g];
-#pragma unroll
-        for (int w = 0; w < NW; w++) mn = fmaxf(mn, red[g][w]);
-        // Logits of -inf alone leave the reference at -inf: as softmax has it, NaN.
-        keep[g] = m[g] == kNegInf ? 0.f : exp2f(m[g] - mn);
-        m[g] = mn;
-        prob[g][tid] = key < seen ? exp2f(x[g] - mn) : 0.f;
-      }
-    __syncthreads();
-    const int keys = (int)min((long)kThreads, seen - c0);
-#pragma unroll
-    for (int g = 0; g < kMaxG; g++)
-      if (g < G) {
-        o[g] *= keep[g];
-        den[g] *= keep[g];
-      }
-    for (int j = kg; j < keys; j += KG) {
-      const long kj = c0 + j;
-      float v;
-      if (kj < n) {
-        const char *tile = ctx + kj / Q::KEYS * Q::BYTES;
-        const int kt = (int)(kj % Q::KEYS), at = Q::vparam(kt, d / Q::GROUP);
-        const uint32_t b = (uint8_t)tile[Q::vbyte(kt, d / 2)];
-        v = fmaf(f16_at(tile + Q::VS + at), (float)(d & 1 ? b >> 4 : b & 15u), f16_at(tile + Q::VZ + at));
-      } else {
-        v = as_f32(V.row((int)(kj - n), D)[d]);
-      }
-#pragma unroll
-      for (int g = 0; g < kMaxG; g++)
-        if (g < G) {
-          const float w = prob[g][j];
-          o[g] = fmaf(w, v, o[g]);
-          den[g] += w;
-        }
+      float4_t *to = reinterpret_cast<float4_t *>(&(val ? vt : kt)[k][ch * 8]);
+      to[0] = (float4_t){x[0], x[1], x[2], x[3]};
+      to[1] = (float4_t){x[4], x[5], x[6], x[7]};
     }
     __syncthreads();
+    // Logits of key `key` and rows rg, rg + 8; a row's 32 are in one half wave.
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const int r = rg + 8 * h;
+      float4_t a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+      for (int i = 0; i < D / 4; i++) {
+        const float4_t x = reinterpret_cast<const float4_t *>(kt[key])[i];
+        const float4_t y = reinterpret_cast<const float4_t *>(qs[r])[i];
+#pragma unroll
+        for (int j = 0; j < 4; j++) a[j] = fmaf(x[j], y[j], a[j]);
+      }
+      const bool seen = key < live && first + key < row_lim[r];
+      const float x = seen ? ((a[0] + a[1]) + (a[2] + a[3])) * p.scale * kLog2e : kNegInf;
+      float m = x;
+#pragma unroll
+      for (int k = 16; k >= 1; k >>= 1) m = fmaxf(m, shfl_xor(m, k));
+      const float was = row_m[r], mn = fmaxf(was, m), ref = mn == kNegInf ? 0.f : mn;
+      const float e = seen ? exp2f(x - ref) : 0.f;
+      float sum = e;
+#pragma unroll
+      for (int k = 16; k >= 1; k >>= 1) sum += shfl_xor(sum, k);
+      prob[r][key] = e;
+      if (key == 0) {
+        const float f = was == kNegInf ? 0.f : exp2f(was - mn);
+        row_f[r] = f;
+        row_m[r] = mn;
+        row_l[r] = row_l[r] * f + sum;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RPT; i++) o[i] *= row_f[kg * RPT + i];
+    if (first + kVecKeys <= sees_all) {
+#pragma unroll 4
+      for (int k = 0; k < kVecKeys; k++) {
+        const float v = vt[k][d];
+#pragma unroll
+        for (int i = 0; i < RPT; i++) o[i] = fmaf(prob[kg * RPT + i][k], v, o[i]);
+      }
+    } else {
+      // A row takes nothing from keys it does not see, whatever they hold.
+      for (int k = 0; k < live; k++) {
+        const float v = vt[k][d];
+#pragma unroll
+        for (int i = 0; i < RPT; i++)
+          o[i] = first + k < row_lim[kg * RPT + i] ? fmaf(prob[kg * RPT + i][k], v, o[i]) : o[i];
+      }
+    }
   }
-  // The KG partial sums of a column.
-  float *part = &prob[0][0];
+  __syncthreads();
 #pragma unroll
-  for (int g = 0; g < kMaxG; g++)
-    if (g < G) {
-      part[tid] = o[g];
-      part[kThreads + tid] = den[g];
-      __syncthreads();
-      if (kg == 0) {
-        float a = 0.f, b = 0.f;
-#pragma unroll
-        for (int k = 0; k < KG; k++) {
-          a += part[k * D + d];
-          b += part[kThreads + k * D + d];
-        }
-        put(static_cast<T *>(p.out) + (qrow + (size_t)g * p.nq) * D + d, seen > 0 ? a / b : 0.f);
+  for (int i = 0; i < RPT; i++) {
+    const int r = kg * RPT + i;
+    if (r >= nrow) continue;
+    if (p.shares == 1) {
+      static_cast<float *>(p.out)[((size_t)unit * per + r0 + r) * D + d] = row_l[r] == 0.f ? 0.f : o[i] / row_l[r];
+    } else {
+      float *rec = p.ws + ((size_t)blockIdx.x * kVecRows + r) * kVecRec<D>;
+      rec[4 + d] = o[i];
+      if (d == 0) {
+        rec[0] = row_m[r];
+        rec[1] = row_l[r];
       }
-      __syncthreads();
     }
+  }
 }
 
+// The records of one row's shares; one thread per column.
+template <int D>
+__global__ __launch_bounds__(D) void quant_vector_join(QuantAttnParams p) {
+  const int blocks = vector_blocks(p), per = p.nq * p.G;
+  const int unit = blockIdx.x / per, row = blockIdx.x % per, d = threadIdx.x;
+  const float *rec = p.ws + (((size_t)unit * blocks + row / kVecRows) * p.shares * kVecRows + row % kVecRows) * kVecRec<D>;
+  const size_t pitch = (size_t)kVecRows * kVecRec<D>;
+  float m = kNegInf, den = 0.f, o = 0.f;
+  for (int k = 0; k < p.shares; k++) m = fmaxf(m, rec[k * pitch]);
+  const float ref = m == kNegInf ? 0.f : m;
+#pragma unroll 4
+  for (int k = 0; k < p.shares; k++) {
+    const float l = rec[k * pitch + 1], f = l == 0.f ? 0.f : exp2f(rec[k * pitch] - ref);
+    den = fmaf(l, f, den);
+    o = fmaf(rec[k * pitch + 4 + d], f, o);
+  }
+  static_cast<float *>(p.out)[((size_t)unit * per + row) * D + d] = den == 0.f ? 0.f : o / den;
+}
 
 // ---------------------------------------------------------------------------
 // bfloat16: matrix products straight from the codes.
@@ -327,10 +362,14 @@ template <int N>
 __device__ __forceinline__ void wait_vm() {
   static_assert(N >= 0 && N < 64, "vmcnt field");
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+  asm volatile("" ::: "memory");  // no read of LDS moves before it
 }
 
 // s_waitcnt lgkmcnt(0): this wave's reads of LDS have been answered.
-__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4)); }
+__device__ __forceinline__ void wait_lds() {
+  __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));
+  asm volatile("" ::: "memory");
+}
 
 // A wave's ring of tiles in LDS. A tile is one block of memory, loaded as it
 // lies by LOADS instructions of 1 KiB (past the end of a unit: zeros, without
@@ -1206,8 +1245,17 @@ constexpr int kChipSimds = 1024;  // 256 CUs of four
 constexpr int kMinSpan = 2;
 constexpr int kMaxBlocks = 4;     // row blocks a wave takes at once
 
-// Plan of a bfloat16 call, from shapes alone.
+// Plan of a call, from shapes alone.
 void plan(QuantAttnParams *p) {
+  if (p->dtype == 0) {
+    // float32: shares of at least four chunks, up to 1024 workgroups.
+    const long groups = (long)p->S * p->L * p->Hkv * vector_blocks(*p);
+    const long chunks = p->ntiles + (p->ocap + kVecKeys - 1) / kVecKeys;
+    const long most = chunks / 4 < 64 ? chunks / 4 : 64, want = 1024 / groups;
+    const long n = want < most ? want : most;
+    p->shares = n < 1 ? 1 : (int)n;
+    return;
+  }
   const int rows = p->C * p->nq * p->G, blocks = (rows + 15) / 16;
   p->row_groups = (blocks + kMaxBlocks - 1) / kMaxBlocks;
   p->rb = (blocks + p->row_groups - 1) / p->row_groups;
@@ -1251,8 +1299,10 @@ void launch_bf16(const QuantAttnParams &p, hipStream_t stream) {
 template <int D, int NG>
 void launch_any(const QuantAttnParams &p, hipStream_t stream) {
   if (p.dtype == 0) {
-    const dim3 grid((uint32_t)p.S * p.L * p.Hkv * p.nq);
-    hipLaunchKernelGGL((quant_attn_vector<float, D, NG>), grid, dim3(kThreads), 0, stream, p);
+    const uint32_t units = (uint32_t)p.S * p.L * p.Hkv;
+    hipLaunchKernelGGL((quant_attn_vector<D, NG>), dim3(units * vector_blocks(p) * p.shares), dim3(kThreads), 0, stream,
+                       p);
+    if (p.shares > 1) hipLaunchKernelGGL((quant_vector_join<D>), dim3(units * p.nq * p.G), dim3(D), 0, stream, p);
   } else {
     launch_bf16<D, NG>(p, stream);
   }
@@ -1261,9 +1311,12 @@ void launch_any(const QuantAttnParams &p, hipStream_t stream) {
 }  // namespace
 
 size_t quant_attn_workspace_bytes(const QuantAttnParams &params) {
-  if (params.dtype == 0) return 0;
   QuantAttnParams p = params;
   plan(&p);
+  if (p.dtype == 0) {
+    if (p.shares == 1) return 0;
+    return (size_t)p.S * p.L * p.Hkv * vector_blocks(p) * p.shares * kVecRows * (4 + p.D) * sizeof(float);
+  }
   // A wave's piece of a unit has record wave + unit.
   const size_t pieces = (size_t)p.nwaves + (size_t)p.P * p.L * p.Hkv;
   return (cut_floats(p.P) + pieces * p.C * p.nq * p.G * (4 + p.D / 2)) * sizeof(float);

@@ -500,14 +500,14 @@ class QuantCache:
 
     def c(self) -> c_quant_cache:
         S, L, Hkv = self.data.shape[:3]
-        assert self.data.is_contiguous() and self.data.dtype == torch.uint8
+        assert self.data.is_cuda and self.data.is_contiguous() and self.data.dtype == torch.uint8
         cc = c_quant_cache(self.data.data_ptr(), S, L, Hkv, self.cap, self.D, self.group)
         assert int(lib.kvr_quant_cache_bytes(ctypes.byref(cc))) == self.data.numel()
         return cc
 
 
 def _ints(t: Optional[torch.Tensor], n: int):
-    assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n)
+    assert t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and t.numel() == n)
     return _ptr(t)
 
 
@@ -546,7 +546,7 @@ def quant_attn(ctx: QuantCache, ctx_len: torch.Tensor, q: torch.Tensor, out: tor
     oc = own.c() if own is not None else None
     S = oc.S if oc else qc.S
     for t in (q, out, k_new, v_new, workspace):
-        assert t is None or t.is_contiguous()
+        assert t is None or (t.is_cuda and t.is_contiguous())
     nq = q.shape[3]
     assert q.shape == out.shape and q.dtype == out.dtype and q.shape[0] == S and q.shape[1] == qc.L \
         and q.shape[4] == qc.D
@@ -573,15 +573,15 @@ def verify_draft(logits: torch.Tensor, draft_tokens: torch.Tensor, sampler: Samp
     """kvr_verify_draft: logits[S * (T + 1)][ld] and draft_logits[S * T][ldd] (None: looked-up tokens) over
     draft_tokens[S][T]; accepted[S], tokens[S][T + 1] and, with len_, len_out[S] are written."""
     S, T = draft_tokens.shape
-    assert logits.dim() == 2 and logits.stride(1) == 1 and logits.shape[0] == S * (T + 1)
+    assert logits.is_cuda and logits.dim() == 2 and logits.stride(1) == 1 and logits.shape[0] == S * (T + 1)
     if draft_logits is not None:
         assert draft_logits.dim() == 2 and draft_logits.stride(1) == 1 and draft_logits.shape[0] == S * T
-        assert draft_logits.dtype == logits.dtype
+        assert draft_logits.is_cuda and draft_logits.dtype == logits.dtype
         Vd = draft_logits.shape[1] if Vd is None else Vd
     V = logits.shape[1] if V is None else V
     for t, n in ((u_accept, S * T), (u_draw, S)):
-        assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n
-    assert workspace is None or workspace.is_contiguous()
+        assert t.dtype == torch.float32 and t.is_cuda and t.is_contiguous() and t.numel() == n
+    assert workspace is None or (workspace.is_cuda and workspace.is_contiguous())
     rc = lib.kvr_verify_draft(_ptr(logits), V, logits.stride(0), _ptr(draft_logits), Vd or 0,
                               0 if draft_logits is None else draft_logits.stride(0), dtype_code(logits.dtype), S, T,
                               _ints(draft_tokens, S * T), _ints(n_draft, S), ctypes.byref(sampler.c()),

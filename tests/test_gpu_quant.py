@@ -234,6 +234,21 @@ def test_attention(case, dtype, new):
     run_attn(case, dtype, new)
 
 
+@pytest.mark.parametrize("D,group", [(128, 32), (128, 64), (64, 32), (64, 64)])
+@pytest.mark.parametrize("G,nq", [(5, 1), (5, 4), (5, 8), (5, 12)])
+def test_every_number_of_row_blocks(G, nq, D, group):
+    """One to four blocks of 16 query rows in each layout, over tiles that are full, cut and crossed."""
+    run_attn((2, 1, 2, G, 2, D, group, nq, [259, 31], [nq, nq + 30]), BF, True)
+    run_attn((2, 1, 2, G, 2, D, group, nq, [259, 31], None), BF, False)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_more_contexts_than_lanes(dtype):
+    lens = [(37 * i * i) % 201 if i % 9 else 0 for i in range(150)]
+    run_attn((150, 1, 2, 3, 1, 64, 32, 1, lens, [1 + i % 40 for i in range(150)]), dtype, True)
+    run_attn((150, 2, 1, 2, 2, 64, 64, 2, lens, [2 + i % 5 for i in range(300)]), dtype, False)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_attention_of_sharp_and_of_flat_logits(dtype):
     # Logits of +-100 (one key decides) and of 0 (all count alike).
@@ -440,3 +455,14 @@ def test_context_past_4_gib():
     want = read(small, 1, 50, ints([50]))
     torch.cuda.synchronize()
     assert torch.equal(dst.k[0, 0, 0, cap - 50:], want.k[0, 0, 0]) and torch.equal(dst.v[0, 0, 0, cap - 50:], want.v[0, 0, 0])
+    # Attention over the rows at the front of the last context.
+    k.quant_append(c, ints([0] * P), src, src_index=ints([0] * P), count=ints([0] * (P - 1) + [50]))
+    q = normal((P, 1, 6, 1, 128), 120).to(DEV)
+    for dtype in (BF, F32):
+        qd, out = q.to(dtype), torch.empty(q.shape, dtype=dtype, device=DEV)
+        ws = torch.empty(k.quant_attn_workspace_size(c, None, 6, 1, dtype) + 16, dtype=torch.uint8, device=DEV)
+        k.quant_attn(c, ints([0] * (P - 1) + [50]), qd, out, 0.09, workspace=ws)
+        torch.cuda.synchronize()
+        assert (out[:P - 1] == 0).all()
+        kk, vv = as_f64(want.k)[0, 0, 0], as_f64(want.v)[0, 0, 0]
+        check(as_f64(out)[P - 1, 0], oq.attend(kk, vv, as_f64(qd)[P - 1, 0], 0.09), np.abs(vv).max(), dtype, "4 GiB")
