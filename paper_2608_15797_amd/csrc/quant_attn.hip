@@ -394,13 +394,13 @@ __device__ __forceinline__ void load_tile(char *slot, const char *tile, bool liv
 #endif  // the host pass has no buffer-to-LDS loads
 }
 
-// With three row blocks and more the keys' values themselves are expanded, z +
+// With three row blocks the keys' values themselves are expanded, z +
 // s n as float16 (off by 2^-12 of an element at most): 15 packed instructions
 // per eight elements against five for the codes, but per key and row one fma
 // after the product instead of two and one per group. 16 contexts shared by 8
 // candidates of 6 heads 348 -> 321 us, 35 rows 328 -> 297.
 template <int RB>
-constexpr bool kKeyValues = RB >= 3;
+constexpr bool kKeyValues = RB == 3;
 
 // The query operands of one row block and what is summed for it.
 template <int D, int NG>
@@ -663,13 +663,13 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
   }
 }
 
-// Waves per SIMD and tiles in a wave's ring. One wave's registers hold up to
-// three row blocks beside another's at D = 128, a fourth of one at D = 64 (18.2
-// us against 18.7 with two waves for 61 contexts of up to 2000); two waves' rings of four 5 KiB tiles each
-// are all of a CU's LDS. 32 contexts of 16384 in groups of 64: rings of two,
-// three and four tiles 620, 656 and 588 us, three waves with two tiles 590.
-constexpr int ctx_waves(int D, int RB) { return RB > 3 ? 1 : D == 128 || RB == 3 ? 2 : RB == 2 ? 3 : 4; }
-constexpr int ctx_depth(int RB) { return RB <= 2 ? 4 : RB == 3 ? 3 : 6; }
+// Waves per SIMD and tiles in a wave's ring. Registers hold two waves of up to
+// three row blocks at D = 128, more of fewer at D = 64 (18.2 us against 18.7
+// for 61 contexts of up to 2000). Two waves' rings of four 5 KiB tiles are all
+// of a CU's LDS: 32 contexts of 16384 in groups of 64 take 620, 656 and 588 us
+// with rings of two, three and four tiles, 590 with three waves of two.
+constexpr int ctx_waves(int D, int RB) { return D == 128 || RB == 3 ? 2 : RB == 2 ? 3 : 4; }
+constexpr int ctx_depth(int RB) { return RB <= 2 ? 4 : 3; }
 
 // Context kernel: one wave per span.
 template <int D, int NG, int RB>
@@ -1243,7 +1243,10 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
 
 constexpr int kChipSimds = 1024;  // 256 CUs of four
 constexpr int kMinSpan = 2;
-constexpr int kMaxBlocks = 4;     // row blocks a wave takes at once
+// Row blocks a wave takes at once; more rows go to further waves over the same
+// tiles. A fourth (one wave per SIMD) took 266 us where two waves of two blocks
+// take 230, for 64 rows over 16 contexts of 8192 x 28 heads at D = 128.
+constexpr int kMaxBlocks = 3;
 
 // Plan of a call, from shapes alone.
 void plan(QuantAttnParams *p) {
@@ -1286,8 +1289,7 @@ void launch_bf16(const QuantAttnParams &p, hipStream_t stream) {
   switch (p.rb) {
     case 1: launch_ctx<D, NG, 1>(p, stream); break;
     case 2: launch_ctx<D, NG, 2>(p, stream); break;
-    case 3: launch_ctx<D, NG, 3>(p, stream); break;
-    default: launch_ctx<D, NG, 4>(p, stream); break;
+    default: launch_ctx<D, NG, 3>(p, stream); break;
   }
   const int per = p.nq * p.G, rpw = p.join_waves ? 16 : p.rpw;
   const dim3 groups((uint32_t)p.S * p.L * p.Hkv * ((per + rpw - 1) / rpw));
