@@ -19,6 +19,11 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int D>
 constexpr int kTileWaves = D / 32;
 
+// New rows per unit up to which a thread takes eight values of a row instead of
+// a workgroup a tile. Lone tokens of 1792 units: 3.0 us against 6.9, eight 5.5
+// against 11.8; 16 rows of 7168 units: 31 against 43, 32 rows 58 against 57.
+constexpr int kFewRows = 16, kRowThreads = 256;
+
 // Eight consecutive values of a row, as loaded.
 template <typename T>
 struct Raw8;
@@ -49,17 +54,20 @@ struct Raw8<float> {
   }
 };
 
+// Read-back values, past the caches: 28 x 2 x 64 units of 150 rows (275 MB of
+// values) take 46 us one after another against 64 with ordinary stores; where
+// the caches are full of another kernel's writes, 75 against 73.
 __device__ __forceinline__ void store8(bf16_t *p, const float (&x)[8]) {
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; i++) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-  *reinterpret_cast<u32x4 *>(p) = w;
+  __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
 }
 __device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
 #pragma unroll
   for (int h = 0; h < 2; h++) {
     const float4_t w = {x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
-    reinterpret_cast<float4_t *>(p)[h] = w;
+    __builtin_nontemporal_store(w, reinterpret_cast<float4_t *>(p) + h);
   }
 }
 
@@ -134,6 +142,38 @@ __device__ __forceinline__ void bounds(const float (&x)[4][8], float (&lo)[4], f
   }
 }
 
+// Scale and offset of a group with these bounds.
+struct Group {
+  f16_t sh, zh;
+  float z, inv;
+  __device__ __forceinline__ Group(float lo, float hi) {
+    zh = (f16_t)lo;
+    z = (float)zh;
+    const float span = hi - z;
+    float step = span * (1.0f / 15.0f);
+    asm volatile("" : "+v"(step));  // rounded to float32 here: no product straight into float16
+    sh = span > 0.f ? (f16_t)step : (f16_t)0.f;
+    const float sc = (float)sh;
+    inv = sc > 0.f ? 1.0f / sc : 0.f;
+  }
+};
+
+// The codes of eight values, the first in the low bits.
+__device__ __forceinline__ uint32_t codes(const float (&x)[8], float z, float inv) {
+  uint32_t b[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    // Adding 2^23 rounds to a whole number, ties to even, in the low bits.
+    const float u = __builtin_amdgcn_fmed3f((x[i] - z) * inv, 0.f, 15.f);
+    b[i] = __float_as_uint(u + 8388608.0f);
+  }
+  uint32_t t[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++) t[i] = (b[2 * i + 1] << 4) | b[2 * i];  // the low byte: two codes
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[3], t[2], 0x0c0c0400u),
+                               __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0400u), 0x05040100u);
+}
+
 // Writes a tile's rows [j0, j1), K by the first waves and V by the others. A
 // workgroup per tile of 32 slots that a unit's new rows may touch; a lane
 // quantises 32 values, and computes the scale and offset of one group for its
@@ -202,30 +242,13 @@ __global__ __launch_bounds__(kTileWaves<D> *kWave) void quant_append_kernel(Quan
     mlo = q == c ? lo[c] : mlo;
     mhi = q == c ? hi[c] : mhi;
   }
-  const f16_t zh = (f16_t)mlo;
-  const float z = (float)zh, span = mhi - z;
-  float step = span * (1.0f / 15.0f);
-  asm volatile("" : "+v"(step));  // rounded to float32 here: no product straight into float16
-  const f16_t sh = span > 0.f ? (f16_t)step : (f16_t)0.f;
-  const float sc = (float)sh, inv = sc > 0.f ? 1.0f / sc : 0.f;
-  const float zc[4] = {quad<0x00>(z), quad<0x55>(z), quad<0xaa>(z), quad<0xff>(z)};
-  const float ic[4] = {quad<0x00>(inv), quad<0x55>(inv), quad<0xaa>(inv), quad<0xff>(inv)};
+  const Group grp(mlo, mhi);
+  const f16_t sh = grp.sh, zh = grp.zh;
+  const float zc[4] = {quad<0x00>(grp.z), quad<0x55>(grp.z), quad<0xaa>(grp.z), quad<0xff>(grp.z)};
+  const float ic[4] = {quad<0x00>(grp.inv), quad<0x55>(grp.inv), quad<0xaa>(grp.inv), quad<0xff>(grp.inv)};
   uint32_t w[4];
 #pragma unroll
-  for (int c = 0; c < 4; c++) {
-    uint32_t b[8];
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      // Adding 2^23 rounds to a whole number, ties to even, in the low bits.
-      const float u = __builtin_amdgcn_fmed3f((x[c][i] - zc[c]) * ic[c], 0.f, 15.f);
-      b[i] = __float_as_uint(u + 8388608.0f);
-    }
-    uint32_t t[4];
-#pragma unroll
-    for (int i = 0; i < 4; i++) t[i] = (b[2 * i + 1] << 4) | b[2 * i];  // the low byte: two codes
-    w[c] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[3], t[2], 0x0c0c0400u),
-                                 __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0400u), 0x05040100u);
-  }
+  for (int c = 0; c < 4; c++) w[c] = codes(x[c], zc[c], ic[c]);
 
   char *out = static_cast<char *>(p.data) + ((size_t)unit * p.ntiles + tile) * Q::BYTES;
   // Scale and offset of chunk q's group, once per group.
@@ -273,7 +296,59 @@ __global__ __launch_bounds__(kTileWaves<D> *kWave) void quant_append_kernel(Quan
   }
 }
 
-// A workgroup per tile of a destination's live slots. A wave loads a KiB of codes, in the append's lanes, and the scales and offsets of its quads'
+// The same for few rows per unit: a thread per eight values, the rows of the
+// units one after another, so that no lane waits for rows that are not there.
+template <typename T, int D, int NG>
+__global__ __launch_bounds__(kRowThreads) void quant_append_rows(QuantAppendParams p) {
+  using Q = QTile<D, NG>;
+  constexpr int CH = D / 8, LANES = Q::GROUP / 8;
+  const size_t it = (size_t)blockIdx.x * kRowThreads + threadIdx.x;
+  const int c = (int)(it % CH);
+  const bool val = it / CH % 2;
+  const size_t row = it / (2 * CH);  // ((s * L + l) * Hkv + h) * T + t
+  const int lh = p.L * p.Hkv;
+  const int unit = (int)(row / p.T), t = (int)(row % p.T), s = unit / lh;
+  if (s >= p.S) return;  // whole groups
+  const int from = p.src_index ? p.src_index[s] : s;
+  const int n = max(p.len[s], 0);
+  const int count = p.count ? min(p.count[s], p.T) : p.T;
+  if (from < 0 || from >= p.S_src || t >= count || (long)n + t >= p.cap) return;
+  const T *src = static_cast<const T *>(val ? p.v : p.k) + (((size_t)from * lh + unit % lh) * p.T + t) * D + c * 8;
+  Raw8<T> raw;
+  raw.load(src);
+  float x[8];
+  raw.get(x);
+  float lo = 0.f, hi = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    x[i] = storable(x[i]);
+    lo = i ? lesser(lo, x[i]) : x[i];
+    hi = i ? greater(hi, x[i]) : x[i];
+  }
+#pragma unroll
+  for (int m = 1; m < LANES; m <<= 1) {
+    lo = lesser(lo, shfl_xor(lo, m));
+    hi = greater(hi, shfl_xor(hi, m));
+  }
+  const Group grp(lo, hi);
+  const uint32_t w = codes(x, grp.z, grp.inv);
+  const int key = (n + t) % Q::KEYS;
+  char *out = static_cast<char *>(p.data) + ((size_t)unit * p.ntiles + (n + t) / Q::KEYS) * Q::BYTES;
+  if (!val) {
+    *reinterpret_cast<uint32_t *>(out + Q::kword(key, c)) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++) out[Q::vbyte(key, c * 4 + i)] = (char)(w >> (8 * i));
+  }
+  if (c % LANES == 0) {
+    const int at = val ? Q::vparam(key, c / LANES) : Q::kparam(key, c / LANES);
+    *reinterpret_cast<f16_t *>(out + (val ? Q::VS : Q::KS) + at) = grp.sh;
+    *reinterpret_cast<f16_t *>(out + (val ? Q::VZ : Q::KZ) + at) = grp.zh;
+  }
+}
+
+// A workgroup per tile of a destination's live slots. A wave loads a KiB of
+// codes, in the append's lanes, and the scales and offsets of its quads'
 // groups; through LDS a lane gets the words, each with its group's scale and
 // offset, of four chunks such that a store covers whole lines (64-byte pieces
 // of 16 rows, as the codes lie, take 509 us for 4096 rows of 28 x 8 x 4 heads).
@@ -348,6 +423,12 @@ __global__ __launch_bounds__(kTileWaves<D> *kWave) void quant_read_kernel(QuantR
 
 template <typename T, int D, int NG>
 void append_launch(const QuantAppendParams &p, hipStream_t stream) {
+  if (p.T <= kFewRows) {
+    const size_t threads = (size_t)p.S * p.L * p.Hkv * p.T * 2 * (D / 8);
+    hipLaunchKernelGGL((quant_append_rows<T, D, NG>), dim3((uint32_t)((threads + kRowThreads - 1) / kRowThreads)),
+                       dim3(kRowThreads), 0, stream, p);
+    return;
+  }
   // T rows touch at most this many tiles of 32, whatever the first one's place.
   const int tiles = (p.T - 1 + kQuantTile - 1) / kQuantTile + 1;
   const uint32_t units = (uint32_t)p.S * p.L * p.Hkv;

@@ -135,6 +135,33 @@ def test_append_of_unusual_values():
             assert torch.isfinite(g).all() and torch.equal(g.cpu(), want)
 
 
+@pytest.mark.parametrize("D,group", [(128, 32), (128, 64), (64, 32), (64, 64)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rows_appended_a_few_at_a_time_are_the_same_bytes(dtype, D, group):
+    k = kvr()
+    S, L, Hkv, T = 3, 2, 5, 57
+    x = [normal((S, L, Hkv, T, D), 50 + i, dtype) for i in range(2)]
+    for y in x:
+        y[:, :, 0, 3, 7], y[:, :, 1, 20, 9], y[:, :, 1, 21, 10] = float("nan"), float("inf"), float("-inf")
+        y[:, :, 2, 30] *= 1e30
+        y[:, :, 3, 40] = -0.0
+        y[:, :, 3, 41, ::2] = 0.0
+        y[:, :, 3, 41, 1::2] = -0.0
+        y[:, :, 4, 42] = float("nan")
+    x = [y.to(DEV) for y in x]
+    start = ints([0, 9, 40])
+    whole = garbage(k.QuantCache.empty(S, L, Hkv, 90, D, group), 3)
+    parts = garbage(k.QuantCache.empty(S, L, Hkv, 90, D, group), 3)
+    assert torch.equal(whole.data, parts.data)
+    k.quant_append(whole, start, k.Cache(*x))
+    a = 0
+    for n in (1, 2, 16, 3, 17, 8, 10):
+        k.quant_append(parts, start + a, k.Cache(*(y[:, :, :, a:a + n].contiguous() for y in x)))
+        a += n
+    torch.cuda.synchronize()
+    assert a == T and torch.equal(whole.data, parts.data)
+
+
 def build(P, L, Hkv, D, group, lens, cap, seed, dtype=BF):
     """A context cache whose unwritten slots are garbage, and its values."""
     k = kvr()
