@@ -819,10 +819,12 @@ __device__ __forceinline__ OwnUnit own_unit(const QuantAttnParams &p, int unit, 
 }
 
 // The rows of a chunk that are in the cache; the bounds check takes the whole
-// offset, so a chunk's place goes into the base.
+// offset, so a chunk's place goes into the base. A chunk reads 32 rows, so a
+// buffer of those is enough, and its bytes fit 32 bits in any cache.
 template <int D>
 __device__ __forceinline__ rsrc_t held_rows(const bf16_t *rows, const OwnUnit &w, int key0) {
-  return make_rsrc(rows + (size_t)key0 * D, (uint32_t)max(w.first - key0, 0) * (2 * D));
+  // A scalar: bounds in vector registers would put a loop around every load.
+  return make_rsrc(rows + (size_t)key0 * D, (uint32_t)uniform(min(max(w.first - key0, 0), 32)) * (2 * D));
 }
 
 // ONE: a single query token, so at most one new row, the last: its lanes' words

@@ -493,3 +493,21 @@ def test_context_past_4_gib():
         assert (out[:P - 1] == 0).all()
         kk, vv = as_f64(want.k)[0, 0, 0], as_f64(want.v)[0, 0, 0]
         check(as_f64(out)[P - 1, 0], oq.attend(kk, vv, as_f64(qd)[P - 1, 0], 0.09), np.abs(vv).max(), dtype, "4 GiB")
+
+
+def test_own_cache_of_rows_past_4_gib():
+    """2^24 + 100 own rows of 256 bytes; those that carry the weight are read where all that are left are 4 GiB."""
+    k = kvr()
+    n, lo, hi = (1 << 24) + 100, 70, 100
+    own = k.Cache(torch.zeros((1, 1, 1, n, 128), dtype=BF, device=DEV), torch.zeros((1, 1, 1, n, 128), dtype=BF, device=DEV))
+    v = normal((hi - lo, 128), 130)
+    own.k[0, 0, 0, lo:hi] = 0.5                      # logits of 40 among zeros: 30 e^40 to 2^24
+    own.v[0, 0, 0, lo:hi] = v.to(DEV)
+    c = k.QuantCache.empty(1, 1, 1, 32, 128, 32)
+    q = torch.ones((1, 1, 2, 1, 128), dtype=BF, device=DEV)
+    out = torch.empty_like(q)
+    ws = torch.empty(k.quant_attn_workspace_size(c, own, 2, 1, BF), dtype=torch.uint8, device=DEV)
+    k.quant_attn(c, ints([0]), q, out, 40.0 / 64, own=own, len_=ints([n]), workspace=ws)
+    torch.cuda.synchronize()
+    want = as_f64(v).mean(0)
+    check(as_f64(out)[0, 0], np.broadcast_to(want, (2, 1, 128)), np.abs(as_f64(v)).max(), BF, "long own")
