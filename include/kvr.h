@@ -475,6 +475,8 @@ int kvr_append(const kvr_cache *cache, const int32_t *len, int32_t T, const void
  *           of codes and 256 D / group of scales and offsets. The sequences i,
  *           i + 1, .. of a cache are a cache of their own that starts i *
  *           bytes / S further on.
+ *   cap   : at most 2^31 - 64 slots, for attention those of the own cache
+ *           included.
  *   group : 32 or 64 consecutive values of a row share a scale and an offset.
  *
  * A group with values x (a NaN taken as 0, all clamped to +-16384; every step

@@ -547,12 +547,18 @@ int kvr_decode_attn_entropy_sample(const kvr_cache *cache, const kvr_prefix *pre
 
 namespace {
 
+constexpr int kQuantMaxSlots = 2147483647 - 63;  // the slots of a last tile have numbers, too
+
+// A launch of `groups` workgroups counts its threads in 32 bits.
+bool past_grid(double groups, int threads) { return groups * threads > 4294967295.0; }
+
 int check_quant(const kvr_quant_cache *c) {
   if (!c) return fail(KVR_EINVAL, "quant cache is NULL");
   if (c->S <= 0 || c->L <= 0 || c->Hkv <= 0 || c->cap <= 0)
     return fail(KVR_EINVAL, "quant cache dims must be positive (S=%d L=%d Hkv=%d cap=%d)", c->S, c->L, c->Hkv, c->cap);
   if (c->D != 64 && c->D != 128) return fail(KVR_EUNSUPPORTED, "head_dim %d is not 64 or 128", c->D);
   if (c->group != 32 && c->group != 64) return fail(KVR_EUNSUPPORTED, "group %d is not 32 or 64", c->group);
+  if (c->cap > kQuantMaxSlots) return fail(KVR_EUNSUPPORTED, "cap=%d slots exceed 2^31 - 64", c->cap);
   if ((double)c->S * c->L * c->Hkv > 2147483647.0) return fail(KVR_EUNSUPPORTED, "S*L*Hkv exceeds the launch grid");
   return KVR_OK;
 }
@@ -605,6 +611,11 @@ int quant_attn_shapes(const kvr_quant_cache *ctx, const kvr_cache *own, int32_t 
   if ((double)p->P * p->L * p->Hkv * p->ntiles > 2147483647.0)
     return fail(KVR_EUNSUPPORTED, "the contexts hold more than 2^31 tiles of 32 slots");
   if ((double)p->S * p->L * Hq * nq > 2147483647.0) return fail(KVR_EUNSUPPORTED, "S*L*Hq*nq exceeds the launch grid");
+  // A workgroup (float32) or a wave per unit and 16 of its rows.
+  if (past_grid((double)p->S * p->L * p->Hkv * ((p->G * nq + 15) / 16), dtype == KVR_F32 ? 256 : 64))
+    return fail(KVR_EUNSUPPORTED, "%d query rows of S*L*Hkv units exceed the launch grid", p->G * nq);
+  if ((double)p->cap + p->ocap > (double)kQuantMaxSlots)
+    return fail(KVR_EUNSUPPORTED, "%d slots of a context and %d of its own exceed 2^31 - 64", p->cap, p->ocap);
   return KVR_OK;
 }
 
@@ -628,7 +639,7 @@ int kvr_quant_append(const kvr_quant_cache *dst, const int32_t *len, const kvr_c
   if (!src_index && src->S != dst->S)
     return fail(KVR_EINVAL, "src has S=%d, dst S=%d, and there is no src_index", src->S, dst->S);
   const double groups = (double)dst->S * dst->L * dst->Hkv * ((double)(src->cap / kvr::kQuantTile) + 2);
-  if (groups > 2147483647.0) return fail(KVR_EUNSUPPORTED, "%d rows of %d units exceed the launch grid", src->cap,
+  if (past_grid(groups, 2 * dst->D)) return fail(KVR_EUNSUPPORTED, "%d rows of %d units exceed the launch grid", src->cap,
                                          dst->S * dst->L * dst->Hkv);
   kvr::QuantAppendParams p{};
   p.data = dst->data; p.S = dst->S; p.L = dst->L; p.Hkv = dst->Hkv; p.cap = dst->cap; p.D = dst->D;
@@ -648,7 +659,7 @@ int kvr_quant_read(const kvr_quant_cache *src, const kvr_cache *dst, const int32
   if (!src_index && src->S != dst->S)
     return fail(KVR_EINVAL, "src has S=%d, dst S=%d, and there is no src_index", src->S, dst->S);
   const double groups = (double)dst->S * dst->L * dst->Hkv * ((double)quant_tiles(dst->cap) + 1);
-  if (groups > 2147483647.0) return fail(KVR_EUNSUPPORTED, "%d slots of %d units exceed the launch grid", dst->cap,
+  if (past_grid(groups, 2 * dst->D)) return fail(KVR_EUNSUPPORTED, "%d slots of %d units exceed the launch grid", dst->cap,
                                          dst->S * dst->L * dst->Hkv);
   kvr::QuantReadParams p{};
   p.data = src->data; p.S_src = src->S; p.L = src->L; p.Hkv = src->Hkv; p.cap = src->cap; p.D = src->D;

@@ -74,6 +74,40 @@ def test_grid_limits():
     assert kvr.lib.kvr_quant_read(B(qc(**big)), B(cc(S=1 << 14, L=1 << 10, Hkv=64, cap=64)), None, 16, None) == EUNSUP
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T", [1, 2, 16, 17, 64])
+def test_launches_of_more_threads_than_32_bits_are_refused(T, D):
+    # A tile of 32 slots takes 2 D threads; T rows touch up to T // 32 + 2 tiles.
+    units = -(-2 ** 32 // (2 * D * (T // 32 + 2)))
+    c = dict(S=units, L=1, Hkv=1, D=D)
+    assert kvr.lib.kvr_quant_append(B(qc(cap=32, **c)), 16, B(cc(cap=T, **c)), None, None, None) == EUNSUP
+    units = -(-2 ** 32 // (2 * D * ((T + 31) // 32 + 1)))
+    c = dict(S=units, L=1, Hkv=1, D=D)
+    assert kvr.lib.kvr_quant_read(B(qc(cap=32, **c)), B(cc(cap=T, **c)), None, 16, None) == EUNSUP
+    # Attention: a wave (float32: four) per unit and 16 of its rows.
+    for dtype, waves in ((0, 4), (1, 1)):
+        blocks = (4 * min(T, 64) + 15) // 16
+        own = cc(S=-(-2 ** 26 // (waves * blocks)), L=1, Hkv=1, D=D, dtype=dtype)
+        args = (B(qc(S=1, L=1, Hkv=1, D=D)), B(own), dtype, 4, T)
+        assert kvr.lib.kvr_quant_attn_workspace_size(*args) == 0 and "grid" in last()
+        own.S -= 1
+        if dtype:
+            assert kvr.lib.kvr_quant_attn_workspace_size(*args) > 0
+
+
+def test_slots_past_31_bits_are_refused():
+    top = 2 ** 31 - 64
+    for cap in (top + 1, 2 ** 31 - 1):
+        c = qc(S=1, L=1, Hkv=1, cap=cap)
+        assert kvr.lib.kvr_quant_cache_bytes(B(c)) == 0 and "2^31" in last()
+        assert kvr.lib.kvr_quant_append(B(c), 16, B(cc(S=1, L=1, Hkv=1)), None, None, None) == EUNSUP
+    assert kvr.lib.kvr_quant_cache_bytes(B(qc(S=1, L=1, Hkv=1, cap=top))) == (top + 31) // 32 * 32 * 160
+    one = dict(S=1, L=1, Hkv=1)
+    f = kvr.lib.kvr_quant_attn_workspace_size
+    assert f(B(qc(cap=top - 50, **one)), B(cc(cap=50, **one)), 1, 4, 1) > 0
+    assert f(B(qc(cap=top - 50, **one)), B(cc(cap=51, **one)), 1, 4, 1) == 0 and "2^31" in last()
+
+
 def attn(own=None, **kw):
     d = dict(ctx_len=16, len=None, q=16, dtype=1, Hq=4, nq=1, scale=1.0, kn=None, vn=None, pos=None, out=16, ws=None,
              nb=0)
