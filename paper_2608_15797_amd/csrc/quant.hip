@@ -57,18 +57,15 @@ struct Raw8<float> {
 // Read-back values, past the caches: 28 x 2 x 64 units of 150 rows (275 MB of
 // values) take 46 us one after another against 64 with ordinary stores; where
 // the caches are full of another kernel's writes, 75 against 73.
-__device__ __forceinline__ void store8(bf16_t *p, const float (&x)[8]) {
+__device__ __forceinline__ void store16(bf16_t *p, const float (&x)[8]) {
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; i++) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
   __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
 }
-__device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
-#pragma unroll
-  for (int h = 0; h < 2; h++) {
-    const float4_t w = {x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
-    __builtin_nontemporal_store(w, reinterpret_cast<float4_t *>(p) + h);
-  }
+__device__ __forceinline__ void store16(float *p, const float (&x)[4]) {
+  const float4_t w = {x[0], x[1], x[2], x[3]};
+  __builtin_nontemporal_store(w, reinterpret_cast<float4_t *>(p));
 }
 
 // A NaN becomes 0 and an infinity the limit: a group has no code for them, and
@@ -403,21 +400,23 @@ __global__ __launch_bounds__(kTileWaves<D> *kWave) void quant_read_kernel(QuantR
     words[wave][e + (e >> 4) * 4] = c4[c];  // four words of padding in 16 keep the banks apart
   }
   wave_sync();
+  // 16 bytes of values per lane and store: a word's eight codes, float32: half of them.
+  constexpr int VALS = 16 / sizeof(T), HALVES = 8 / VALS;
 #pragma unroll
-  for (int c = 0; c < 4; c++) {
-    const int e = c * kWave + lane;
-    const uint32_t word = words[wave][e + (e >> 4) * 4], pz = params[wave][e / LANES];
+  for (int c = 0; c < 4 * HALVES; c++) {
+    const int e = (c * kWave + lane) / HALVES, half = (c * kWave + lane) % HALVES;
+    const uint32_t word = words[wave][e + (e >> 4) * 4] >> (half * 16), pz = params[wave][e / LANES];
     const float sc = (float)__builtin_bit_cast(f16_t, (uint16_t)pz);
     const float z = (float)__builtin_bit_cast(f16_t, (uint16_t)(pz >> 16));
     const uint32_t even = word & 0x0f0f0f0fu, odd = (word >> 4) & 0x0f0f0f0fu;
-    float x[8];
+    float x[VALS];
 #pragma unroll
-    for (int m = 0; m < 4; m++) {
+    for (int m = 0; m < VALS / 2; m++) {
       x[2 * m] = fmaf(sc, (float)((even >> (8 * m)) & 0xffu), z);
       x[2 * m + 1] = fmaf(sc, (float)((odd >> (8 * m)) & 0xffu), z);
     }
     const int j = tile * Q::KEYS + key0 + (e >> log_cpr);
-    if (j < end) store8(out + (size_t)j * D + d0 + (e & ((1 << log_cpr) - 1)) * 8, x);
+    if (j < end) store16(out + (size_t)j * D + d0 + (e & ((1 << log_cpr) - 1)) * 8 + half * VALS, x);
   }
 }
 
