@@ -222,7 +222,7 @@ struct QuantAttnParams {
   // Plan of a bfloat16 call: row blocks per wave and groups of them, waves of
   // the context kernel and their least span in tiles, rows per workgroup of
   // the join, or a wave each.
-  int rb, row_groups, nwaves, min_span, rpw, join_waves;
+  int rb, row_groups, nwaves, rpw, join_waves;
   int shares;  // of a float32 call's keys
 };
 size_t quant_attn_workspace_bytes(const QuantAttnParams &p);

@@ -217,9 +217,10 @@ __global__ __launch_bounds__(D) void quant_vector_join(QuantAttnParams p) {
   const float *rec = p.ws + (((size_t)unit * blocks + row / kVecRows) * p.shares * kVecRows + row % kVecRows) * kVecRec<D>;
   const size_t pitch = (size_t)kVecRows * kVecRec<D>;
   float m = kNegInf, den = 0.f, o = 0.f;
+#pragma unroll 8
   for (int k = 0; k < p.shares; k++) m = fmaxf(m, rec[k * pitch]);
   const float ref = m == kNegInf ? 0.f : m;
-#pragma unroll 4
+#pragma unroll 8
   for (int k = 0; k < p.shares; k++) {
     const float l = rec[k * pitch + 1], f = l == 0.f ? 0.f : exp2f(rec[k * pitch] - ref);
     den = fmaf(l, f, den);
@@ -335,7 +336,7 @@ __device__ __forceinline__ Cut cut_of(const QuantAttnParams &p, int lane) {
   for (int c0 = kWave; c0 < p.P; c0 += kWave)
     sum += lane_value(scan_lanes(ctx_tiles(p, c0 + lane)), kWave - 1);
   cut.total = sum * p.L * p.Hkv;
-  cut.span = max((int)(((uint32_t)cut.total + p.nwaves - 1) / (uint32_t)p.nwaves), p.min_span);
+  cut.span = max((int)(((uint32_t)cut.total + p.nwaves - 1) / (uint32_t)p.nwaves), 1);
   return cut;
 }
 
@@ -1243,8 +1244,7 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
     put_row<EL>(static_cast<bf16_t *>(p.out) + ((size_t)unit * per + r0 + row) * D, sub, o, den);
 }
 
-constexpr int kChipSimds = 1024;  // 256 CUs of four
-constexpr int kMinSpan = 2;
+constexpr int kChipCus = 256, kChipSimds = 4 * kChipCus;
 // Row blocks a wave takes at once; more rows go to further waves over the same
 // tiles. A fourth (one wave per SIMD) took 266 us where two waves of two blocks
 // take 230, for 64 rows over 16 contexts of 8192 x 28 heads at D = 128.
@@ -1253,10 +1253,11 @@ constexpr int kMaxBlocks = 3;
 // Plan of a call, from shapes alone.
 void plan(QuantAttnParams *p) {
   if (p->dtype == 0) {
-    // float32: shares of at least four chunks, up to 1024 workgroups.
+    // float32: shares of the chunks, up to 1024 workgroups. 32 units of 2 and 3
+    // chunks: 26 us with one chunk each, 31 with two, 44 with all.
     const long groups = (long)p->S * p->L * p->Hkv * vector_blocks(*p);
     const long chunks = p->ntiles + (p->ocap + kVecKeys - 1) / kVecKeys;
-    const long most = chunks / 4 < 64 ? chunks / 4 : 64, want = 1024 / groups;
+    const long most = chunks < 64 ? chunks : 64, want = 1024 / groups;
     const long n = want < most ? want : most;
     p->shares = n < 1 ? 1 : (int)n;
     return;
@@ -1267,16 +1268,15 @@ void plan(QuantAttnParams *p) {
   const double tiles = (double)p->P * p->L * p->Hkv * p->ntiles;
   const int waves = kChipSimds * ctx_waves(p->D, p->rb);
   const int most = waves / p->row_groups > 64 ? waves / p->row_groups : 64;
-  p->min_span = kMinSpan;
-  const double want = tiles / kMinSpan + 1;
-  p->nwaves = want < most ? (int)want : most;
+  p->nwaves = tiles < most ? (int)tiles : most;
   // The join: a wave each where that fills the chip; else workgroups, of
-  // fewer rows where there are few of them.
+  // fewer rows where they stay one per CU (each reads all the own rows: 132
+  // units of 12 rows 13.6 us, 17 with twice as many, 27 with four times).
   const int per = p->nq * p->G;
   const long units = (long)p->S * p->L * p->Hkv;
   p->join_waves = units * ((per + 15) / 16) >= kChipSimds;
   int rpw = 16;
-  while (rpw > 1 && units * ((per + rpw - 1) / rpw) < 512) rpw /= 2;
+  while (rpw > 1 && units * ((per + rpw / 2 - 1) / (rpw / 2)) <= kChipCus) rpw /= 2;
   p->rpw = rpw;
 }
 
