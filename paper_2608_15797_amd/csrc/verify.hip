@@ -15,6 +15,8 @@
 // the positions.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "entropy_common.h"
 #include "kvr_device.h"
 #include "kvr_internal.h"
@@ -217,39 +219,84 @@ struct Dist {
   double p;
 };
 
-// The k best keys of the row's splits, sorted over the lanes, by one wave. The
-// largest of the splits' k-th keys bounds the row's k-th from below (the split
-// that has it has k); what reaches it is ranked by counting, after a bitwise
-// search for the k-th key where that is more than a wave's lanes.
-template <int NPL>
-__device__ __forceinline__ uint64_t merge_keys(const VerifyParams &p, int r, int k, int lane, uint64_t *tmp) {
+// The word of lane ^ M, without LDS (a workgroup's waves merge at once).
+template <int M>
+__device__ __forceinline__ uint32_t exchange(uint32_t x) {
+  auto dpp = [](uint32_t v, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, decltype(ctrl)::value, 0xf, 0xf, true);
+  };
+  if constexpr (M == 1) return dpp(x, std::integral_constant<int, 0xb1>());
+  if constexpr (M == 2) return dpp(x, std::integral_constant<int, 0x4e>());
+  // Lane ^ 3 within four lanes, lane ^ 7 within eight.
+  if constexpr (M == 4) return dpp(dpp(x, std::integral_constant<int, 0x1b>()), std::integral_constant<int, 0x141>());
+  if constexpr (M == 8) return dpp(x, std::integral_constant<int, 0x128>());  // by 8 around 16
+#if defined(__HIP_DEVICE_COMPILE__)
+  // The rows (halves) of x and of its copy change places: one holds the even ones twice, one the odd.
+  const bool odd = threadIdx.x & M;
+  if constexpr (M == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return odd ? r[0] : r[1];
+  }
+  if constexpr (M == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return odd ? r[0] : r[1];
+  }
+#endif
+  return x;
+}
+
+// Keys M lanes apart in order: the larger first, with `up` last.
+template <int M>
+__device__ __forceinline__ uint64_t order(uint64_t x, bool up) {
+  const uint64_t o = exchange<M>((uint32_t)x) | ((uint64_t)exchange<M>((uint32_t)(x >> 32)) << 32);
+  const bool less = ((threadIdx.x & M) != 0) != up;  // this lane takes the smaller one
+  return (x < o) == less ? x : o;
+}
+
+// Runs of SIZE lanes that fall and then rise (or rise and then fall), sorted:
+// rising where `up` says so.
+template <int SIZE>
+__device__ __forceinline__ uint64_t sort_runs(uint64_t x, bool up) {
+  if constexpr (SIZE >= 64) x = order<32>(x, up);
+  if constexpr (SIZE >= 32) x = order<16>(x, up);
+  if constexpr (SIZE >= 16) x = order<8>(x, up);
+  if constexpr (SIZE >= 8) x = order<4>(x, up);
+  if constexpr (SIZE >= 4) x = order<2>(x, up);
+  return order<1>(x, up);
+}
+
+// The k best keys of the row's splits, sorted over the lanes, by one wave. A
+// register holds as many of the splits' sorted lists as fit its lanes, every
+// other one rising, and is sorted from there; NB registers are then joined in
+// pairs, one falling and one rising: the larger of each lane's two keys are the
+// best of both.
+template <int NB>
+__device__ __forceinline__ uint64_t merge_keys(const VerifyParams &p, int r, int k, int lane) {
   const uint64_t *src = list_at(p, r, 0);
-  const int kmax = max(p.top_k, p.top_kd), all = p.splits * k;
-  uint64_t v[NPL];
+  const int kmax = max(p.top_k, p.top_kd);
+  const int log_kp = k > 1 ? 32 - __clz(k - 1) : 0, kp = 1 << log_kp;  // lanes of a list
+  uint64_t best = 0;
+  for (int s0 = 0; s0 < p.splits; s0 += NB * kWave >> log_kp) {
+    uint64_t v[NB];
 #pragma unroll
-  for (int i = 0; i < NPL; i++) {
-    const int e = lane + i * kWave;
-    v[i] = e < all ? src[(size_t)(e / k) * kmax + e % k] : 0;
+    for (int i = 0; i < NB; i++) {
+      const int e = i * kWave + lane, split = s0 + (e >> log_kp);
+      const int at = (e >> log_kp) & 1 ? kp - 1 - (e & (kp - 1)) : e & (kp - 1);
+      v[i] = split < p.splits && at < k ? src[(size_t)split * kmax + at] : 0;
+    }
+#define KVR_SORT(SIZE)                                                                                    \
+    if (kp < SIZE)                                                                                        \
+      _Pragma("unroll") for (int i = 0; i < NB; i++) v[i] = sort_runs<SIZE>(v[i], (i * kWave + lane) & SIZE);
+    KVR_SORT(2) KVR_SORT(4) KVR_SORT(8) KVR_SORT(16) KVR_SORT(32) KVR_SORT(64)
+#undef KVR_SORT
+#pragma unroll
+    for (int n = NB / 2; n >= 1; n /= 2)
+#pragma unroll
+      for (int i = 0; i < n; i++)
+        v[i] = sort_runs<kWave>(max(v[2 * i], v[2 * i + 1]), n > 1 ? i & 1 : s0 > 0);
+    best = s0 == 0 ? v[0] : sort_runs<kWave>(max(best, v[0]), false);
   }
-  uint64_t bound = 1;
-#pragma unroll
-  for (int i = 0; i < NPL; i++) {
-    const int e = lane + i * kWave;
-    if (e < all && e % k == k - 1) bound = max(bound, v[i]);
-  }
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) bound = max(bound, (uint64_t)__shfl_xor((unsigned long long)bound, m, kWave));
-  if (wave_count_ge<NPL>(v, bound) > kWave) bound = select_threshold<NPL>(v, k, kWave);
-  wave_lds_sync();
-  const int n = wave_store_ge<NPL>(tmp, v, bound, lane);
-  wave_lds_sync();
-  const uint64_t key = lane < n ? tmp[lane] : 0;
-  int rank = 0;
-  for (int j = 0; j < n; j++) rank += tmp[j] > key;
-  wave_lds_sync();
-  if (lane < n) tmp[rank] = key;
-  wave_lds_sync();
-  return lane < n && lane < k ? tmp[lane] : 0;
+  return lane < k ? best : 0;
 }
 
 __device__ __forceinline__ double lane_cumsum(double x, int lane) {
@@ -277,24 +324,23 @@ __device__ __forceinline__ Dist distribution(uint64_t key, double temp, double t
 }
 
 // The lists of a sequence's rows, a wave per row; then one wave goes through the
-// positions. NPL: keys per lane of a merge.
-template <int NPL>
+// positions. NB: registers of lists merged at once.
+template <int NB>
 __global__ __launch_bounds__(kMergeWaves * kWave) void verify_walk(VerifyParams p) {
   extern __shared__ char lds[];
   __shared__ int stands[kWave];  // T is at most 32
   const int s = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int nd = p.n_draft ? min(max(p.n_draft[s], 0), p.T) : p.T;
-  // Probabilities and ids of the target's rows, then of the draft's; scratch of the merges.
+  // Probabilities and ids of the target's rows, then of the draft's.
   const int rows = 2 * p.T + 1;
   double *prob = reinterpret_cast<double *>(lds);
   int *ids = reinterpret_cast<int *>(prob + (size_t)rows * kWave);
-  uint64_t *tmp = reinterpret_cast<uint64_t *>(ids + (size_t)rows * kWave) + wave * kWave;
   const int live = nd + 1 + (p.draft ? nd : 0);
   for (int i = wave; i < live; i += kMergeWaves) {
     const bool draft = i > nd;
     const int t = draft ? i - nd - 1 : i;
     const int r = draft ? p.S * (p.T + 1) + s * p.T + t : s * (p.T + 1) + t;
-    const uint64_t key = merge_keys<NPL>(p, r, draft ? p.top_kd : p.top_k, lane, tmp);
+    const uint64_t key = merge_keys<NB>(p, r, draft ? p.top_kd : p.top_k, lane);
     const Dist d = distribution(key, draft ? p.tempd : p.temp, draft ? p.top_pd : p.top_p, lane);
     const int at = (draft ? p.T + 1 + t : t) * kWave + lane;
     prob[at] = d.p;
@@ -387,11 +433,14 @@ hipError_t launch_verify_draft(const VerifyParams &params, hipStream_t stream) {
   else launch_rows<bf16_t>(p, grid, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const size_t lds = (size_t)(2 * p.T + 1) * kWave * (sizeof(double) + sizeof(int)) +
-                     (size_t)kMergeWaves * kWave * sizeof(uint64_t);
+  const size_t lds = (size_t)(2 * p.T + 1) * kWave * (sizeof(double) + sizeof(int));
   const dim3 seqs(p.S), threads(kMergeWaves * kWave);
-  if (p.splits * k <= 4 * kWave) hipLaunchKernelGGL(verify_walk<4>, seqs, threads, lds, stream, p);
-  else hipLaunchKernelGGL(verify_walk<kListMax / kWave>, seqs, threads, lds, stream, p);
+  int lanes = 1;  // of a list
+  while (lanes < k) lanes *= 2;
+  const int regs = (p.splits * lanes + kWave - 1) / kWave;
+  if (regs <= 2) hipLaunchKernelGGL(verify_walk<2>, seqs, threads, lds, stream, p);
+  else if (regs <= 4) hipLaunchKernelGGL(verify_walk<4>, seqs, threads, lds, stream, p);
+  else hipLaunchKernelGGL(verify_walk<8>, seqs, threads, lds, stream, p);
   return hipGetLastError();
 }
 
