@@ -840,7 +840,7 @@ __device__ __forceinline__ void load_keys(OwnChunk<D> &c, const OwnUnit &w, int 
 #pragma unroll
     for (int i = 0; i < D / 32; i++)
       c.k[t][i] = __builtin_amdgcn_raw_buffer_load_b128(held, n * ROW + g * 16 + t * 16 * ROW + i * 64, 0, kStreamLoad);
-  if (key0 + 32 <= w.first || w.first == w.u) return;
+  if (key0 + 32 <= w.first || key0 >= w.u || w.first == w.u) return;
   const rsrc_t fresh = make_rsrc(w.fk, w.nq * ROW);
   if constexpr (ONE) {
     const int key = w.first - key0;
@@ -848,12 +848,14 @@ __device__ __forceinline__ void load_keys(OwnChunk<D> &c, const OwnUnit &w, int 
     u32x4 x[D / 32];
 #pragma unroll
     for (int i = 0; i < D / 32; i++) x[i] = __builtin_amdgcn_raw_buffer_load_b128(fresh, off + i * 64, 0, kStreamLoad);
+    // Masks, not branches: a load that one path does not take up is waited for
+    // where the paths meet, and with it the loads before.
 #pragma unroll
-    for (int t = 0; t < 2; t++)
-      if (t == key >> 4) {
+    for (int t = 0; t < 2; t++) {
+      const uint32_t mask = t == key >> 4 ? ~0u : 0u;
 #pragma unroll
-        for (int i = 0; i < D / 32; i++) c.k[t][i] |= x[i];
-      }
+      for (int i = 0; i < D / 32; i++) c.k[t][i] |= x[i] & mask;
+    }
   } else {
     // Rows before the first new one get an offset past the end.
 #pragma unroll
@@ -884,18 +886,18 @@ __device__ __forceinline__ void load_values(OwnChunk<D> &c, const OwnUnit &w, in
   const rsrc_t held = held_rows<D>(w.v, w, key0);
 #pragma unroll
   for (int e = 0; e < 8; e++) get(held, slot_key(g, e) * ROW, c.v[e], false);
-  if (key0 + 32 <= w.first || w.first == w.u) return;
+  if (key0 + 32 <= w.first || key0 >= w.u || w.first == w.u) return;
   const rsrc_t fresh = make_rsrc(w.fv, w.nq * ROW);
   if constexpr (ONE) {
     const int key = w.first - key0, slot = 4 * (key >> 4) + (key & 3);
     uint32_t x[D / 32];
     get(fresh, g == ((key >> 2) & 3) ? 0u : 0x40000000u, x, false);
 #pragma unroll
-    for (int e = 0; e < 8; e++)
-      if (e == slot) {
+    for (int e = 0; e < 8; e++) {
+      const uint32_t mask = e == slot ? ~0u : 0u;
 #pragma unroll
-        for (int i = 0; i < D / 32; i++) c.v[e][i] |= x[i];
-      }
+      for (int i = 0; i < D / 32; i++) c.v[e][i] |= x[i] & mask;
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; e++) get(fresh, (uint32_t)((key0 + slot_key(g, e) - w.first) * ROW), c.v[e], true);
@@ -973,7 +975,7 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
       top = fmaxf(top, x[t][j]);
     }
   }
-  if (next < w.u) load_keys<D, ONE>(ch, w, next, lane);
+  load_keys<D, ONE>(ch, w, next, lane);
   top = fmaxf(top, shfl_xor(top, 16));
   top = fmaxf(top, shfl_xor(top, 32));
   const float mn = fmaxf(st.m, top), ref = mn == kNegInf ? 0.f : mn;
@@ -1023,7 +1025,7 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
       const u32x4 v = value_operand<D>(ch.v, b);
       st.o[b] = mfma_bf16(lo, v, mfma_bf16(hi, v, st.o[b]));
     }
-    if (next < w.u) load_values<D, ONE>(ch, w, next, lane);
+    load_values<D, ONE>(ch, w, next, lane);
     return;
   }
 #pragma unroll 1
@@ -1045,7 +1047,7 @@ __device__ __forceinline__ void own_step(OwnState<D> &st, OwnChunk<D> &ch, const
       for (int j = 0; j < 4; j++) st.o[b][j] = (w.r0 + 4 * g + j) % w.nq == t ? acc[j] : st.o[b][j];
     }
   }
-  if (next < w.u) load_values<D, ONE>(ch, w, next, lane);
+  load_values<D, ONE>(ch, w, next, lane);
 }
 
 // The chunks key0, key0 + stride, .. of a unit. A chunk's keys make way for the
@@ -1107,9 +1109,10 @@ __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(ONE ? 3 :
   const OwnUnit w = own_unit<D>(p, unit, u, r0, nrow);
   OwnChunk<D> ch;
   if (u > 0) {
+    // The queries first: a wait for them in the loop would be one for all before.
+    own_begin<D>(st, p, w, unit, lane);
     load_keys<D, ONE>(ch, w, 0, lane);
     load_values<D, ONE>(ch, w, 0, lane);
-    own_begin<D>(st, p, w, unit, lane);
   }
   const Records here = records_of(p, plan, unit % lh);
   own_attend<D, ONE>(st, ch, w, 0, 32, lane);
@@ -1157,7 +1160,7 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
   const int per = p.nq * p.G, blocks = (per + p.rpw - 1) / p.rpw;
   const int unit = blockIdx.x / blocks, r0 = blockIdx.x % blocks * p.rpw;
   const int lh = p.L * p.Hkv, s = unit / lh, c = s / p.C;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, n = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), n = lane & 15, g = lane >> 4;
   const RecordPlan plan(p, c);
   const int u = uniform(own_len(p, s)), nrow = min(p.rpw, per - r0);
 
@@ -1165,9 +1168,9 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
   OwnState<D> st;
   OwnChunk<D> ch;
   if (u > 0) {
+    own_begin<D>(st, p, w, unit, lane);
     load_keys<D, false>(ch, w, wave * 32, lane);
     load_values<D, false>(ch, w, wave * 32, lane);
-    own_begin<D>(st, p, w, unit, lane);
   }
   const Records here = records_of(p, plan, unit % lh);
   if (p.ok && r0 == 0) store_new<bf16_t, D, NT>(p, unit, s, u);
