@@ -1252,6 +1252,11 @@ constexpr int kChipCus = 256, kChipSimds = 4 * kChipCus;
 // tiles. A fourth (one wave per SIMD) took 266 us where two waves of two blocks
 // take 230, for 64 rows over 16 contexts of 8192 x 28 heads at D = 128.
 constexpr int kMaxBlocks = 3;
+// Fewer where tiles x blocks are at most this many times one (two): a wave's
+// chain is shorter, and its tiles come from the L2. 48 rows, one block and
+// three: 512 tiles 13.8 us and 16.9, 3584 25 and 36, 15136 42 (two) and 50;
+// 64512 tiles 145 us with one and 116 with three.
+constexpr double kBlockTiles = 65536;
 
 // Plan of a call, from shapes alone.
 void plan(QuantAttnParams *p) {
@@ -1266,9 +1271,11 @@ void plan(QuantAttnParams *p) {
     return;
   }
   const int rows = p->C * p->nq * p->G, blocks = (rows + 15) / 16;
-  p->row_groups = (blocks + kMaxBlocks - 1) / kMaxBlocks;
-  p->rb = (blocks + p->row_groups - 1) / p->row_groups;
   const double tiles = (double)p->P * p->L * p->Hkv * p->ntiles;
+  int most_blocks = kMaxBlocks;
+  while (most_blocks > 1 && tiles * blocks <= (most_blocks - 1) * kBlockTiles) most_blocks--;
+  p->row_groups = (blocks + most_blocks - 1) / most_blocks;
+  p->rb = (blocks + p->row_groups - 1) / p->row_groups;
   const int waves = kChipSimds * ctx_waves(p->D, p->rb);
   const int most = waves / p->row_groups > 64 ? waves / p->row_groups : 64;
   p->nwaves = tiles < most ? (int)tiles : most;
