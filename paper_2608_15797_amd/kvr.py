@@ -156,7 +156,8 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # current_stream().cuda_stream without the object: 0.3 us of 3.
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -499,10 +500,15 @@ class QuantCache:
         return QuantCache(self.data[a:b], self.cap, self.D, self.group)
 
     def c(self) -> c_quant_cache:
+        cached = self.__dict__.get("_c")
+        if cached is not None and cached[0] is self.data and cached[1] == (self.data.data_ptr(), self.cap, self.D,
+                                                                          self.group):
+            return cached[2]
         S, L, Hkv = self.data.shape[:3]
         assert self.data.is_cuda and self.data.is_contiguous() and self.data.dtype == torch.uint8
         cc = c_quant_cache(self.data.data_ptr(), S, L, Hkv, self.cap, self.D, self.group)
         assert int(lib.kvr_quant_cache_bytes(ctypes.byref(cc))) == self.data.numel()
+        self.__dict__["_c"] = (self.data, (self.data.data_ptr(), self.cap, self.D, self.group), cc)
         return cc
 
 
