@@ -1279,12 +1279,15 @@ void plan(QuantAttnParams *p) {
   const int waves = kChipSimds * ctx_waves(p->D, p->rb);
   const int most = waves / p->row_groups > 64 ? waves / p->row_groups : 64;
   p->nwaves = tiles < most ? (int)tiles : most;
-  // The join: a wave each where that fills the chip; else workgroups, of
-  // fewer rows where they stay one per CU (each reads all the own rows: 132
-  // units of 12 rows 13.6 us, 17 with twice as many, 27 with four times).
+  // The join: a wave per 16 rows where that fills the chip, or is more than a
+  // workgroup per CU with about two records per unit (336 units 10.3 us, 14.4 as
+  // workgroups; with seven records 20 and 16); else workgroups, of fewer rows
+  // where they stay one per CU (each reads all the own rows: 132 units of 12
+  // rows 13.6 us, 17 with twice as many, 27 with four times).
   const int per = p->nq * p->G;
-  const long units = (long)p->S * p->L * p->Hkv;
-  p->join_waves = units * ((per + 15) / 16) >= kChipSimds;
+  const long units = (long)p->S * p->L * p->Hkv, waves16 = units * ((per + 15) / 16);
+  const bool few_records = p->nwaves <= 2.0 * p->P * p->L * p->Hkv;
+  p->join_waves = waves16 >= kChipSimds || (waves16 > kChipCus && few_records);
   int rpw = 16;
   while (rpw > 1 && units * ((per + rpw / 2 - 1) / (rpw / 2)) <= kChipCus) rpw /= 2;
   p->rpw = rpw;
