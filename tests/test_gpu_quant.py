@@ -172,9 +172,18 @@ def build(P, L, Hkv, D, group, lens, cap, seed, dtype=BF):
     return c, [oq.stand_for(r.float().numpy(), group) for r in rows]
 
 
-def check(got, ref, vmax, dtype, what):
+def roomy(ctx, tiles):
+    """The same context at the front of units of that many tiles."""
+    S, L, Hkv, held, _ = ctx.data.shape
+    big = kvr().QuantCache.empty(S, L, Hkv, 32 * tiles, ctx.D, ctx.group)
+    big.data.fill_(0xff)
+    big.data[:, :, :, :held] = ctx.data
+    return big
+
+
+def check(got, ref, vmax, dtype, what, more=0.0):
     err = np.abs(got - ref)
-    tol = 2.0 ** -8 * np.abs(ref) + 8 * 2.0 ** -11 * vmax if dtype == BF else 3e-5 * vmax + 0 * ref
+    tol = 2.0 ** -8 * np.abs(ref) + (8 * 2.0 ** -11 + more) * vmax if dtype == BF else 3e-5 * vmax + 0 * ref
     say(what, "largest error / tolerance %.3f" % (err / np.maximum(tol, 1e-30)).max(),
         "rms error / rms %.2e" % (np.sqrt((err ** 2).mean()) / max(np.sqrt((ref ** 2).mean()), 1e-30)))
     assert np.isfinite(got).all() and (err <= tol).all()
@@ -197,10 +206,12 @@ ATTN = [  # P, C, L, G, Hkv, D, group, nq, context lengths, own lengths (None: n
 ]
 
 
-def run_attn(case, dtype, new, seed=7, scale=None):
+def run_attn(case, dtype, new, seed=7, scale=None, tiles=0):
     P, C, L, G, Hkv, D, group, nq, lens, own = ATTN[case] if isinstance(case, int) else case
     k, S = kvr(), P * C
     ctx, (ck, cv) = build(P, L, Hkv, D, group, lens, max(lens) + 5, seed, dtype)
+    if tiles:                    # the same contexts at the front of units of that many tiles
+        ctx = roomy(ctx, tiles)
     q = normal((S, L, G * Hkv, nq, D), seed + 3, dtype)
     scale = 1.0 / math.sqrt(D) if scale is None else scale
     out = torch.full(q.shape, float("nan"), dtype=dtype, device=DEV)
@@ -267,6 +278,30 @@ def test_every_number_of_row_blocks(G, nq, D, group):
     """One to four blocks of 16 query rows in each layout, over tiles that are full, cut and crossed."""
     run_attn((2, 1, 2, G, 2, D, group, nq, [259, 31], [nq, nq + 30]), BF, True)
     run_attn((2, 1, 2, G, 2, D, group, nq, [259, 31], None), BF, False)
+
+
+@pytest.mark.parametrize("D,group", [(128, 32), (128, 64), (64, 32), (64, 64)])
+@pytest.mark.parametrize("G,nq", [(5, 1), (5, 4), (5, 8), (5, 12), (7, 14)])
+def test_row_blocks_of_a_wave_over_caches_of_many_tiles(G, nq, D, group):
+    """The same rows where room for 65536 tiles and more gives a wave two blocks, and three."""
+    blocks = (G * nq + 15) // 16
+    for room in (90000, 180000):
+        tiles = room // (4 * blocks) + 1
+        run_attn((2, 1, 1, G, 2, D, group, nq, [259, 31], [nq, nq + 30]), BF, True, tiles=tiles)
+        run_attn((1, 2, 1, G, 4, D, group, nq, [300], [nq + 1, nq + 33]), BF, False, tiles=tiles)
+        run_attn((2, 1, 1, G, 2, D, group, nq, [259, 31], None), BF, False, tiles=tiles)
+
+
+@pytest.mark.parametrize("D,group", [(128, 32), (64, 64)])
+@pytest.mark.parametrize("nq", [1, 3])
+@pytest.mark.parametrize("new", [False, True])
+def test_more_units_than_the_chip_has_waves(new, nq, D, group):
+    """1040 units (and 280 of a tile each) of every length, some shorter than the query tokens."""
+    lens, own = [(41 * i) % 75 for i in range(130)], [(29 * i) % 71 for i in range(260)]
+    run_attn((130, 2, 1, 3, 4, D, group, nq, lens, own), BF, new)
+    run_attn((140, 1, 1, 7, 2, D, group, nq, [i % 28 for i in range(140)], own[:140]), BF, new)
+    if not new:
+        run_attn((140, 1, 2, 6, 4, D, group, nq, [i % 28 for i in range(140)], None), BF, False)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -362,6 +397,30 @@ def test_attention_of_small_and_large_queries(std):
     kk = np.concatenate([ck[0][0, 0], as_f64(own.k)[0, 0, 0]])
     vv = np.concatenate([cv[0][0, 0], as_f64(own.v)[0, 0, 0]])
     check(as_f64(out)[0, 0], oq.attend(kk, vv, as_f64(q)[0, 0], sc), np.abs(vv).max(), BF, ("q std", std))
+
+
+@pytest.mark.parametrize("std,qstd,scale", [(1.0, 1.0, 1.0), (1.0, 1.0, 0.0), (1e-4, 1.0, 0.09), (3000.0, 1.0, 0.09),
+                                            (1.0, 1e-6, 2e4), (1.0, 1e4, 2e-6)])
+@pytest.mark.parametrize("G,nq,tiles", [(12, 2, 40000), (16, 3, 50000)])
+@pytest.mark.parametrize("D,group", [(128, 32), (64, 64)])
+def test_unusual_sizes_with_two_and_three_row_blocks(D, group, G, nq, tiles, std, qstd, scale):
+    """Sharp and flat logits, values and queries far from 1. Three blocks take the keys' values as float16: each
+    off by 2^-12 of itself, a logit by that of sum |q k|, and a probability by as much again through the sum."""
+    k = kvr()
+    rows = [normal((1, 1, 1, 333, D), 140, F32), normal((1, 1, 1, 333, D), 141, F32, std)]
+    ctx = k.QuantCache.empty(1, 1, 1, 333, D, group)
+    k.quant_append(ctx, ints([0]), k.Cache(rows[0].to(DEV), rows[1].to(DEV)))
+    ctx = roomy(ctx, tiles)
+    q = normal((1, 1, G, nq, D), 142, BF, qstd)
+    q[..., 7] *= 10.0 if qstd != 1.0 else 1.0
+    out = torch.empty(q.shape, dtype=BF, device=DEV)
+    ws = torch.empty(k.quant_attn_workspace_size(ctx, None, G, nq), dtype=torch.uint8, device=DEV)
+    k.quant_attn(ctx, ints([333]), q.to(DEV), out, scale, workspace=ws)
+    torch.cuda.synchronize()
+    kk, vv = (oq.stand_for(r.numpy(), group)[0, 0, 0] for r in rows)
+    q = as_f64(q)[0, 0]
+    more = 2 * 2.0 ** -12 * scale * (np.abs(q) @ np.abs(kk).T).max() if nq == 3 else 0.0
+    check(as_f64(out)[0, 0], oq.attend(kk, vv, q, scale), np.abs(vv).max(), BF, (D, G * nq, std, qstd, scale), more)
 
 
 def _step(dtype=BF):
