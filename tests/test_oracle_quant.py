@@ -80,3 +80,17 @@ def test_all_tokens_stand_and_the_next_comes_from_the_last_row():
     assert oq.verify(lg, None, [4, 3], 2, [0.99, 0.01], 0.3, smp)[0] == [4, 2]
     assert oq.verify(lg, None, [-1, 3], 2, [0.0, 0.0], 0.3, smp)[0] == [4]
     assert oq.verify(lg, None, [1, 1], 0, [0.0, 0.0], 0.3, smp)[0] == [4]
+
+
+def test_attention_of_the_last_tokens_is_torchs_with_a_shifted_causal_mask():
+    import torch
+    rng = np.random.default_rng(5)
+    for N, nq in ((9, 1), (20, 4), (4, 4)):
+        k, v, q = rng.normal(size=(N, 16)), rng.normal(size=(N, 16)), rng.normal(size=(3, nq, 16))
+        mask = torch.ones(nq, N, dtype=torch.bool).tril(N - nq)
+        t = [torch.from_numpy(x).expand(3, -1, -1) for x in (k, v)]
+        want = torch.nn.functional.scaled_dot_product_attention(torch.from_numpy(q), *t, attn_mask=mask, scale=0.3)
+        assert np.abs(oq.attend(k, v, q, 0.3) - want.numpy()).max() <= 1e-13
+    # Query tokens before the first token see nothing.
+    out = oq.attend(k[:2], v[:2], rng.normal(size=(1, 4, 16)), 0.3)
+    assert (out[0, :2] == 0).all() and np.abs(out[0, 2] - v[0]).max() <= 1e-15
