@@ -281,7 +281,7 @@ def test_every_number_of_row_blocks(G, nq, D, group):
 
 
 @pytest.mark.parametrize("D,group", [(128, 32), (128, 64), (64, 32), (64, 64)])
-@pytest.mark.parametrize("G,nq", [(5, 1), (5, 4), (5, 8), (5, 12), (7, 14)])
+@pytest.mark.parametrize("G,nq", [(5, 1), (5, 4), (5, 8), (5, 12), (7, 14), (5, 30)])
 def test_row_blocks_of_a_wave_over_caches_of_many_tiles(G, nq, D, group):
     """The same rows where room for 65536 tiles and more gives a wave two blocks, and three."""
     blocks = (G * nq + 15) // 16

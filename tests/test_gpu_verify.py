@@ -106,6 +106,16 @@ def test_tokens_counts_and_lengths(S, T, V, Vd, dtype, kind):
     check(x, d, tok, ua, ud, V, Vd, SMP, nd=nd, lens=[100 + s for s in range(S)])
 
 
+@pytest.mark.parametrize("top,dtop", [(1, 2), (2, 1), (3, 9), (9, 17), (17, 33), (33, 5), (64, 20), (20, 64)])
+@pytest.mark.parametrize("V,dtype", [(200003, BF), (400000, F32), (700001, BF)])
+def test_lists_of_many_splits(V, dtype, top, dtop):
+    """Rows long enough for many splits, whose lists fill two merges' registers and more, of every list length."""
+    x, d, tok, ua, ud = inputs(2, 2, V, V - 17, dtype, top * 100 + dtop, "boosted")
+    check(x, d, tok, ua, ud, V, V - 17, (0.9, top, 1.0), (1.1, dtop, 1.0))
+    x, _, tok, ua, ud = inputs(1, 2, V, 0, dtype, top * 100 + dtop + 1, "ties")
+    check(x, None, tok, ua, ud, V, 0, (0.9, top, 1.0))
+
+
 @pytest.mark.parametrize("smp,dsmp", [((1.0, 1, 1.0), None), ((0.3, 64, 1.0), (2.0, 3, 0.5)),
                                       ((1.7, 5, 0.1), (0.8, 64, 0.999))])
 def test_samplers_of_their_own(smp, dsmp):
