@@ -677,8 +677,12 @@ template <int D, int NG, int RB>
 __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(ctx_waves(D, RB)))) void quant_ctx(QuantAttnParams p) {
   using Q = QTile<D, NG>;
   constexpr int DEPTH = ctx_depth(RB), LOADS = Ring<D, NG>::LOADS, SLOT = Ring<D, NG>::SLOT;
-  __shared__ __align__(1024) char ring[DEPTH * SLOT];
-  __shared__ int limits[RB <= 2 ? 1 : RB * 16];  // visible keys of each row, beyond two blocks (registers)
+  // With the ring, beyond two blocks (registers): the visible keys of each row.
+  // One array: of two, the compiler waits for every load into the ring before
+  // it reads any of it (16 contexts shared by 8
+  // candidates of 6 heads 320 us, 288 so).
+  __shared__ __align__(1024) char ring[DEPTH * SLOT + (RB <= 2 ? 0 : RB * 64)];
+  int *limits = reinterpret_cast<int *>(ring + DEPTH * SLOT);
   const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
   // The row groups of a span run eight workgroups apart, on one XCD.
   const int xcd = blockIdx.x & 7, k8 = blockIdx.x >> 3;
