@@ -395,13 +395,13 @@ __device__ __forceinline__ void load_tile(char *slot, const char *tile, bool liv
 #endif  // the host pass has no buffer-to-LDS loads
 }
 
-// With three row blocks the keys' values themselves are expanded, z +
+// With three row blocks and more the keys' values themselves are expanded, z +
 // s n as float16 (off by 2^-12 of an element at most): 15 packed instructions
 // per eight elements against five for the codes, but per key and row one fma
 // after the product instead of two and one per group. 16 contexts shared by 8
 // candidates of 6 heads 348 -> 321 us, 35 rows 328 -> 297.
 template <int RB>
-constexpr bool kKeyValues = RB == 3;
+constexpr bool kKeyValues = RB >= 3;
 
 // The query operands of one row block and what is summed for it.
 template <int D, int NG>
@@ -669,18 +669,18 @@ __device__ __forceinline__ void tile_step(Block<D, NG> (&blk)[RB], const char *s
 // for 61 contexts of up to 2000). Two waves' rings of four 5 KiB tiles are all
 // of a CU's LDS: 32 contexts of 16384 in groups of 64 take 620, 656 and 588 us
 // with rings of two, three and four tiles, 590 with three waves of two.
-constexpr int ctx_waves(int D, int RB) { return D == 128 || RB == 3 ? 2 : RB == 2 ? 3 : 4; }
-constexpr int ctx_depth(int RB) { return RB <= 2 ? 4 : 3; }
+constexpr int ctx_waves(int D, int RB) { return D == 128 || RB >= 3 ? 2 : RB == 2 ? 3 : 4; }
+constexpr int ctx_depth(int D, int RB) { return D == 128 && RB >= 3 ? 3 : 4; }
 
 // Context kernel: one wave per span.
 template <int D, int NG, int RB>
 __global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(ctx_waves(D, RB)))) void quant_ctx(QuantAttnParams p) {
   using Q = QTile<D, NG>;
-  constexpr int DEPTH = ctx_depth(RB), LOADS = Ring<D, NG>::LOADS, SLOT = Ring<D, NG>::SLOT;
+  constexpr int DEPTH = ctx_depth(D, RB), LOADS = Ring<D, NG>::LOADS, SLOT = Ring<D, NG>::SLOT;
   // With the ring, beyond two blocks (registers): the visible keys of each row.
   // One array: of two, the compiler waits for every load into the ring before
-  // it reads any of it (16 contexts shared by 8
-  // candidates of 6 heads 320 us, 288 so).
+  // it reads any of it (16 contexts shared by 8 candidates of 6 heads 320 us,
+  // 288 so).
   __shared__ __align__(1024) char ring[DEPTH * SLOT + (RB <= 2 ? 0 : RB * 64)];
   int *limits = reinterpret_cast<int *>(ring + DEPTH * SLOT);
   const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
@@ -1253,9 +1253,10 @@ __global__ __launch_bounds__(kOwnWaves *kWave) __attribute__((amdgpu_waves_per_e
 
 constexpr int kChipCus = 256, kChipSimds = 4 * kChipCus;
 // Row blocks a wave takes at once; more rows go to further waves over the same
-// tiles. A fourth (one wave per SIMD) took 266 us where two waves of two blocks
-// take 230, for 64 rows over 16 contexts of 8192 x 28 heads at D = 128.
-constexpr int kMaxBlocks = 3;
+// tiles. Two waves per SIMD hold three at D = 128 (a fourth, one wave per SIMD,
+// takes 267 us where two waves of two take 233, for 64 rows over 16 contexts of
+// 8192 x 28 heads), four at D = 64 (131 us as two of two, 121).
+constexpr int max_blocks(int D) { return D == 128 ? 3 : 4; }
 // Fewer where tiles x blocks are at most this many times one (two): a wave's
 // chain is shorter, and its tiles come from the L2. 48 rows, one block and
 // three: 512 tiles 13.8 us and 16.9, 3584 25 and 36, 15136 42 (two) and 50;
@@ -1276,11 +1277,8 @@ void plan(QuantAttnParams *p) {
   }
   const int rows = p->C * p->nq * p->G, blocks = (rows + 15) / 16;
   const double tiles = (double)p->P * p->L * p->Hkv * p->ntiles;
-  int most_blocks = kMaxBlocks;
+  int most_blocks = max_blocks(p->D);
   while (most_blocks > 1 && tiles * blocks <= (most_blocks - 1) * kBlockTiles) most_blocks--;
-  // Five to eight blocks go in pairs: 128 rows 441 -> 431 us (D = 64: 283 -> 241),
-  // 96 rows 333 -> 341 (198 -> 188); nine 434 as threes, 520 as pairs.
-  if (blocks >= 5 && blocks <= 8 && most_blocks == 3) most_blocks = 2;
   p->row_groups = (blocks + most_blocks - 1) / most_blocks;
   p->rb = (blocks + p->row_groups - 1) / p->row_groups;
   const int waves = kChipSimds * ctx_waves(p->D, p->rb);
@@ -1311,7 +1309,9 @@ void launch_bf16(const QuantAttnParams &p, hipStream_t stream) {
   switch (p.rb) {
     case 1: launch_ctx<D, NG, 1>(p, stream); break;
     case 2: launch_ctx<D, NG, 2>(p, stream); break;
-    default: launch_ctx<D, NG, 3>(p, stream); break;
+    case 3: launch_ctx<D, NG, 3>(p, stream); break;
+    default:
+      if constexpr (D == 64) launch_ctx<D, NG, 4>(p, stream);
   }
   const int per = p.nq * p.G, rpw = p.join_waves ? 16 : p.rpw;
   const dim3 groups((uint32_t)p.S * p.L * p.Hkv * ((per + rpw - 1) / rpw));
