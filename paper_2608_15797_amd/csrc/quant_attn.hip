@@ -108,37 +108,53 @@ __global__ __launch_bounds__(kThreads) void quant_attn_vector(QuantAttnParams p)
     const int live = min(kVecKeys, own ? n + u - first : n - first);
     const char *tile = ctx + (size_t)t * Q::BYTES;
     __syncthreads();
-    for (int e = tid; e < 2 * kVecKeys * CH; e += kThreads) {
-      const bool val = e >= kVecKeys * CH;
-      const int k = e / CH % kVecKeys, ch = e % CH;
-      float x[8];
-      if (k >= live) {
+    // A thread's pieces of eight values: all their loads, then the values.
+    constexpr int PIECES = 2 * kVecKeys * CH / kThreads;
+    float x[PIECES][8];
+    if (own) {
+      float4_t w[PIECES][2];
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = 0.f;
-      } else if (own) {
-        const float *row = (val ? V : K).row(first - n + k, D) + ch * 8;
+      for (int i = 0; i < PIECES; i++) {
+        const int e = tid + i * kThreads, k = e / CH % kVecKeys;
+        const float *row = (e >= kVecKeys * CH ? V : K).row(first - n + min(k, live - 1), D) + e % CH * 8;
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-          const float4_t w = reinterpret_cast<const float4_t *>(row)[h];
-#pragma unroll
-          for (int i = 0; i < 4; i++) x[4 * h + i] = w[i];
-        }
-      } else {
-        const int grp = ch * 8 / Q::GROUP, at = val ? Q::VS + Q::vparam(k, grp) : Q::KS + Q::kparam(k, grp);
-        const float sc = f16_at(tile + at), z = f16_at(tile + at + (Q::KZ - Q::KS));
-        uint32_t w = 0;
-        if (!val) {
-          w = *reinterpret_cast<const uint32_t *>(tile + Q::kword(k, ch));
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; i++) w |= (uint32_t)(uint8_t)tile[Q::vbyte(k, ch * 4 + i)] << (8 * i);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = fmaf(sc, (float)((w >> (4 * i)) & 15u), z);
+        for (int h = 0; h < 2; h++) w[i][h] = reinterpret_cast<const float4_t *>(row)[h];
       }
-      float4_t *to = reinterpret_cast<float4_t *>(&(val ? vt : kt)[k][ch * 8]);
-      to[0] = (float4_t){x[0], x[1], x[2], x[3]};
-      to[1] = (float4_t){x[4], x[5], x[6], x[7]};
+#pragma unroll
+      for (int i = 0; i < PIECES; i++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) x[i][j] = w[i][j >> 2][j & 3];
+    } else {
+      uint32_t w[PIECES];
+      float sc[PIECES], z[PIECES];
+#pragma unroll
+      for (int i = 0; i < PIECES; i++) {
+        const int e = tid + i * kThreads, k = e / CH % kVecKeys, ch = e % CH;
+        const bool val = e >= kVecKeys * CH;
+        const int grp = ch * 8 / Q::GROUP, at = val ? Q::VS + Q::vparam(k, grp) : Q::KS + Q::kparam(k, grp);
+        sc[i] = f16_at(tile + at);
+        z[i] = f16_at(tile + at + (Q::KZ - Q::KS));
+        if (!val) {
+          w[i] = *reinterpret_cast<const uint32_t *>(tile + Q::kword(k, ch));
+        } else {
+          w[i] = 0;
+#pragma unroll
+          for (int j = 0; j < 4; j++) w[i] |= (uint32_t)(uint8_t)tile[Q::vbyte(k, ch * 4 + j)] << (8 * j);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < PIECES; i++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) x[i][j] = fmaf(sc[i], (float)((w[i] >> (4 * j)) & 15u), z[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; i++) {
+      const int e = tid + i * kThreads, k = e / CH % kVecKeys;
+#pragma unroll
+      for (int j = 0; j < 8; j++) x[i][j] = k < live ? x[i][j] : 0.f;
+      float4_t *to = reinterpret_cast<float4_t *>(&(e >= kVecKeys * CH ? vt : kt)[k][e % CH * 8]);
+      to[0] = (float4_t){x[i][0], x[i][1], x[i][2], x[i][3]};
+      to[1] = (float4_t){x[i][4], x[i][5], x[i][6], x[i][7]};
     }
     __syncthreads();
     // Logits of key `key` and rows rg, rg + 8; a row's 32 are in one half wave.
