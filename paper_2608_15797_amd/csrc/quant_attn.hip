@@ -161,6 +161,7 @@ __global__ __launch_bounds__(kThreads) void quant_attn_vector(QuantAttnParams p)
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       const int r = rg + 8 * h;
+      if (8 * h >= nrow) break;  // the rows past the last are not stored
       float4_t a = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
       for (int i = 0; i < D / 4; i++) {
